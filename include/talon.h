@@ -42,6 +42,7 @@ extern "C" {
 
 #define TALON_DTYPE_F32 0
 #define TALON_DTYPE_BF16 1
+#define TALON_DTYPE_F16 2   /* the calls on a paged cache only */
 
 /* limits */
 #define TALON_K_MAX 64     /* per-row candidate cap k; the selection also needs (N-1)*k <= 4096 */
@@ -53,6 +54,8 @@ extern "C" {
 #define TALON_STATUS_DONE_DEPTH 2u  /* max_depth layers built before the budget ran out */
 #define TALON_STATUS_BAD_ROW 4u     /* NaN / +inf logit or a row with no finite maximum */
 #define TALON_STATUS_ABORTED 8u     /* a single launch gave up waiting (talon_set_spin_limit_us) */
+
+#define TALON_STATUS_BAD_PAGE 16u   /* a page table entry that names no page, or rows beyond the table (paged cache) */
 
 /* logits row addressing for talon_expand_layer */
 #define TALON_ROWS_BY_NODE 0     /* row of node i of sequence b = i                        */
@@ -470,6 +473,144 @@ int talon_tree_attention_static(const void* q, const void* k_prefix, const void*
                                 int32_t max_prefix_len, int64_t kv_stride_b, int64_t kv_stride_t,
                                 int64_t kv_stride_h, float scale, void* out, float* out_lse,
                                 void* stream);
+
+/* ------------------------------------------------------------------------------------------------
+ * A cache kept in pages.  The calls above verify trees against one slab of prefix rows per sequence; these five
+ * do the same work on a pool of pages, and what a server does around it: they write the new tokens' rows
+ * (rotated), attend with any number of new tokens (one, a tree, a chunk of a prompt), move the accepted path's
+ * rows behind the prefix, add up the attention weight of every row and drop the rows that have least.
+ *
+ * Row r of sequence b lies in page page_table[b][r / page_size], slot r % page_size; element (page, slot, g, :)
+ * of K and of V at page*stride_page + slot*stride_token + g*stride_head elements (Dh contiguous), so tokens of a
+ * page may lie together or its heads.  The rows of new tokens lie in the cache like all others: new token i of
+ * sequence b is row prefix_len[b] + i.  Sequences may share pages that are only read.
+ *
+ * What only the device can see: a table entry outside [0, num_pages), where a row of it is read or written,
+ * and rows beyond the table's max_pages * page_size set TALON_STATUS_BAD_PAGE in status[b].  Nothing outside the
+ * pool is touched; rows that have no place are not written, and a sequence's outputs are not meaningful where
+ * a row of it could not be read.  Lengths outside their bounds are taken as the nearest bound.  No call clears
+ * status.
+ */
+typedef struct talon_paged_cache {
+  int32_t B;                /* sequences, at most TALON_B_MAX                                    */
+  int32_t Hkv, Dh;          /* KV heads (at most 128) and their width (a multiple of 8)          */
+  int32_t dtype;            /* TALON_DTYPE_BF16 or TALON_DTYPE_F16                               */
+  int32_t num_pages;        /* pages of the pool                                                 */
+  int32_t page_size;        /* rows of a page, a power of two                                    */
+  int32_t max_pages;        /* entries of the page table per sequence                            */
+  int64_t stride_page, stride_token, stride_head; /* elements, multiples of 8                    */
+  void *k, *v;              /* the pools, 16-byte aligned, at most 64 GiB each                   */
+  int32_t* page_table;      /* [B][max_pages]                                                    */
+  uint32_t* status;         /* [B] TALON_STATUS_* bits                                           */
+} talon_paged_cache;
+
+/* A caller's tensor [B][N][heads][Dh]: element (b, i, h, :) at b*stride_b + i*stride_t + h*stride_h, Dh contiguous,
+ * 16-byte aligned, strides in elements, multiples of 8 (0 in what is only read: broadcast). */
+typedef struct talon_view {
+  void* data;
+  int64_t stride_b, stride_t, stride_h;
+} talon_view;
+
+/*
+ * What makes a score besides the product (NULL: all of it plain).  For new token i (position p_i) and row j:
+ *   x = scale * q_i . k_j;  softcap > 0: x = softcap * tanh(x / softcap);  slopes: x -= slopes[h] * |p_i - p_j|
+ * p_j = j for rows of the prefix; new token i stands at p_i = prefix_len + offset[i] (a tree: its depth), without
+ * offset at prefix_len + i.  Token i sees row j
+ *   - of the prefix always, of a new token if its mask bit is set (mask [B][N][ceil(N/64)] words, as
+ *     talon_build_tree_mask writes them with N = N_pad; any pattern: a tree, a document, a prefix that sees itself) or,
+ *     without a mask, if it is not later than i;
+ *   - and, with window > 0, only if p_i - p_j < window.
+ * A token that sees nothing gets an output of 0 and a log-denominator of -inf.  What lies in rows, masks and
+ * new tokens that a token does not see has no effect on it, whatever it is (NaN and infinities included); a value of V
+ * that is no finite number and is seen may make the whole output of the row NaN.
+ */
+typedef struct talon_scores {
+  const uint64_t* mask;     /* NULL: causal                                                      */
+  const int32_t* offset;    /* [B][N], a negative one counts as 0; NULL: i                       */
+  const float* slopes;      /* [Hq] or NULL                                                      */
+  float scale;              /* 0: 1/sqrt(Dh)                                                     */
+  float softcap;            /* 0: none                                                           */
+  int32_t window;           /* 0: none                                                           */
+} talon_scores;
+
+/*
+ * The new tokens' queries and keys rotated by their positions, keys and values written into the pages.
+ *   angle(i, f) = (pos_base[b] + pos[axis(f)][b][i]) * inv_freq[f], f = 0 .. pairs-1
+ *   (x1, x2) -> (x1 cos - x2 sin, x2 cos + x1 sin)
+ * with x1 = x[f], x2 = x[f + pairs], or, interleaved, x1 = x[2f], x2 = x[2f + 1]; values from 2*pairs on and all
+ * of v are copied.  axis(f) = pair_axis[f] clamped to [0, axes) (NULL: 0): positions in time, height and width of
+ * an image's tokens each turn their own pairs.
+ *   q, q_out [B][N][Hq][Dh] (q_out may be q: each value is read and written by one thread), k, v [B][N][Hkv][Dh];
+ *   views of one fused tensor are fine.  pos int32 [axes][B][N]; pos_base int32 [B] or NULL; inv_freq float [pairs].
+ *   Tokens i >= n_new[b] are neither read nor written.  Positions are taken in 64 bits, sines and cosines are
+ *   good to fp32, results are rounded once.
+ *   Errors: INVALID_ARG, UNSUPPORTED (dtype, sizes).
+ */
+int talon_rotary_store(const talon_paged_cache* cache, const talon_view* q, const talon_view* k, const talon_view* v,
+                       const talon_view* q_out, int32_t N, int32_t Hq, const int32_t* n_new, const int32_t* prefix_len,
+                       const int32_t* pos, int32_t axes, const int32_t* pos_base, const float* inv_freq, int32_t pairs,
+                       const int32_t* pair_axis, int32_t interleaved, void* stream);
+
+/*
+ * Attention of the new tokens (at most N of every sequence, any number from one on) over the paged cache, the rows
+ * of the new tokens included (write them first).  KV head = h / (Hq/Hkv).
+ *   q, out [B][N][Hq][Dh]; out_lse float [B][N][Hq] or NULL: natural-log softmax denominator.  Rows i >= n_new[b]
+ *   of out and out_lse are untouched.  prefix_len[b] <= max_prefix_len (host bound, sizes the launch).
+ *   Arithmetic: matrix instructions with fp32 accumulation, fp32 online softmax, probabilities rounded to the
+ *   storage type before the product with V, outputs rounded once (partial results of a row are fp32).  Where
+ *   rows are cut depends on all lengths of the batch: the low bits of a sequence's result may differ between
+ *   batches.  The same call on the same data repeats its result bit for bit.
+ *   `workspace`: talon_paged_attention_workspace_bytes bytes, no initialisation needed, not to be shared by calls that
+ *   run at the same time.
+ *   Errors: INVALID_ARG, UNSUPPORTED (Dh other than 64, 128, 256; Hq % Hkv != 0; Hq/Hkv > 128; more than 2^30 key
+ *   tiles), WORKSPACE.
+ */
+size_t talon_paged_attention_workspace_bytes(int32_t B, int32_t N, int32_t Hq, int32_t Hkv, int32_t Dh, int32_t max_prefix_len);
+int talon_paged_attention(const talon_paged_cache* cache, const talon_view* q, int32_t N, int32_t Hq, const int32_t* n_new,
+                          const int32_t* prefix_len, int32_t max_prefix_len, const talon_scores* scores, const talon_view* out,
+                          float* out_lse, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * The attention weight that every row of the cache receives, added up (what talon_paged_evict goes by):
+ *   weights[b][g][j] = decay * prior[b][g][j] (j < prefix_len[b]) + sum over new tokens i and query heads h of
+ *                      KV head g of exp(x_ihj - lse[b][i][h]),   j < prefix_len[b] + n_new[b]
+ * with scores and arguments as in talon_paged_attention and its out_lse; a token whose lse is +inf counts nothing
+ * (a drafted token that was not accepted).  weights, prior float, element (b, g, j) at b*stride_b + g*stride_h + j;
+ * prior may be weights or NULL (0); further rows are untouched.  Sums are fp32, in a fixed order.
+ *   Errors: as talon_paged_attention (no workspace), INVALID_ARG for strides that do not hold max_prefix_len + N rows
+ *   (or the table's rows where those are fewer) and for decay outside [-1, 1].
+ */
+int talon_paged_weights(const talon_paged_cache* cache, const talon_view* q, int32_t N, int32_t Hq, const int32_t* n_new,
+                        const int32_t* prefix_len, int32_t max_prefix_len, const talon_scores* scores, const float* lse,
+                        float decay, const float* prior, float* weights, int64_t stride_b, int64_t stride_h, void* stream);
+
+/*
+ * Eviction: of every sequence with len[b] > budget rows, each KV head keeps its first n_sink rows, its last
+ * n_recent and, of those between, the ones of largest weight until `budget` rows are kept (ties to the lowest row; a
+ * weight that is no number is the least).  The kept rows of K and V move, in their order, to rows 0 .. of dst's
+ * pages (dst NULL or the same pools and table: in place; other pages of the same pools leave the old rows as they
+ * are, which a sequence that shares them still needs; pages of dst must not hold rows of `cache` that are still to be read).
+ *   kept int32 [B][Hkv][budget]: the old row of every new one, -1 beyond; new_len[b] = min(len[b], budget) (may not be
+ *   len).  weights as in talon_paged_weights; new_weights (may be weights, or NULL): the kept rows' weights, in order.
+ *   Shorter sequences keep all rows.  Rows count as positions from then on (offset and slopes are relative to
+ *   rows); what the keys were rotated by stays in them.
+ *   Errors: INVALID_ARG (budget < 1, n_sink + n_recent > budget, dst of another shape or too small, strides).
+ */
+int talon_paged_evict(const talon_paged_cache* cache, const talon_paged_cache* dst, const int32_t* len, int32_t max_len,
+                      const float* weights, int64_t stride_b, int64_t stride_h, int32_t budget, int32_t n_sink,
+                      int32_t n_recent, int32_t* kept, int32_t* new_len, float* new_weights, int64_t new_stride_b,
+                      int64_t new_stride_h, void* stream);
+
+/*
+ * talon_compact_kv for a paged cache: rows prefix_len[b] + path[b][j], j = 0 .. accept_len[b], move to rows
+ * prefix_len[b] + j (path int32 [B][N] and accept_len as talon_greedy_accept writes them; all are read before
+ * one is written), new_prefix_len[b] = prefix_len[b] + accept_len[b] + 1, at most the table's rows (may not be
+ * prefix_len).  weights (optional, as in talon_paged_weights, weight_rows rows each: a row that is not among them stays
+ * where it is) move along.  Errors: INVALID_ARG (N > TALON_N_MAX, ...).
+ */
+int talon_paged_compact(const talon_paged_cache* cache, int32_t N, const int32_t* path, const int32_t* accept_len,
+                        const int32_t* prefix_len, int32_t* new_prefix_len, float* weights, int32_t weight_rows,
+                        int64_t stride_b, int64_t stride_h, void* stream);
 
 #ifdef __cplusplus
 }

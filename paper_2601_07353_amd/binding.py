@@ -27,6 +27,7 @@ TALON_ERR_WORKSPACE = -3
 TALON_ERR_RUNTIME = -4
 TALON_DTYPE_F32 = 0
 TALON_DTYPE_BF16 = 1
+TALON_DTYPE_F16 = 2   # the calls on a paged cache only
 TALON_K_MAX = 64
 TALON_N_MAX = 256
 TALON_B_MAX = 256
@@ -34,6 +35,7 @@ TALON_STATUS_DONE_BUDGET = 1
 TALON_STATUS_DONE_DEPTH = 2
 TALON_STATUS_BAD_ROW = 4
 TALON_STATUS_ABORTED = 8
+TALON_STATUS_BAD_PAGE = 16
 TALON_ROWS_BY_NODE = 0
 TALON_ROWS_BY_FRONTIER = 1
 
@@ -45,6 +47,8 @@ EXPORTS = [
     "talon_greedy_accept", "talon_compact_kv", "talon_prune_tree",
     "talon_build_tree_mask", "talon_tree_attention_workspace_bytes", "talon_tree_attention",
     "talon_static_scratch_bytes", "talon_static_scratch_init", "talon_tree_attention_static",
+    "talon_rotary_store", "talon_paged_attention_workspace_bytes", "talon_paged_attention", "talon_paged_weights",
+    "talon_paged_evict", "talon_paged_compact",
 ]
 
 
@@ -62,13 +66,29 @@ class _CTreeState(Structure):
                 ("depth_cur", c_void_p), ("status", c_void_p)]
 
 
+class _CPagedCache(Structure):
+    _fields_ = [("B", c_int32), ("Hkv", c_int32), ("Dh", c_int32), ("dtype", c_int32), ("num_pages", c_int32),
+                ("page_size", c_int32), ("max_pages", c_int32), ("stride_page", c_int64), ("stride_token", c_int64),
+                ("stride_head", c_int64), ("k", c_void_p), ("v", c_void_p), ("page_table", c_void_p), ("status", c_void_p)]
+
+
+class _CView(Structure):
+    _fields_ = [("data", c_void_p), ("stride_b", c_int64), ("stride_t", c_int64), ("stride_h", c_int64)]
+
+
+class _CScores(Structure):
+    _fields_ = [("mask", c_void_p), ("offset", c_void_p), ("slopes", c_void_p), ("scale", c_float), ("softcap", c_float),
+                ("window", c_int32)]
+
+
 _lib = None
 
 # what csrc/marshal.cpp calls, in its order
 _MARSHALLED = ["talon_last_error_string", "talon_tree_init", "talon_expand_layer", "talon_select_budget", "talon_expand_select_layer",
                "talon_expand_tree", "talon_build_tree", "talon_build_tree_ahead", "talon_expand_literal", "talon_expand_literal_ahead",
                "talon_target_argmax", "talon_greedy_accept", "talon_compact_kv", "talon_build_tree_mask", "talon_tree_attention",
-               "talon_tree_attention_static"]
+               "talon_tree_attention_static", "talon_rotary_store", "talon_paged_attention", "talon_paged_weights", "talon_paged_evict",
+               "talon_paged_compact"]
 
 
 class _Unloaded:
@@ -153,6 +173,14 @@ def load_library() -> ctypes.CDLL:
     lib.talon_static_scratch_init.argtypes = []
     lib.talon_tree_attention_static.argtypes = [P, P, P, P, P, P, P, P, c_int32, c_int32, c_int32, c_int32, c_int32,
                                                 c_int32, c_int64, c_int64, c_int64, c_float, P, P, P]
+    C, W, S = POINTER(_CPagedCache), POINTER(_CView), POINTER(_CScores)
+    lib.talon_rotary_store.argtypes = [C, W, W, W, W, c_int32, c_int32, P, P, P, c_int32, P, P, c_int32, P, c_int32, P]
+    lib.talon_paged_attention_workspace_bytes.restype = c_size_t
+    lib.talon_paged_attention_workspace_bytes.argtypes = [c_int32] * 6
+    lib.talon_paged_attention.argtypes = [C, W, c_int32, c_int32, P, P, c_int32, S, W, P, P, c_size_t, P]
+    lib.talon_paged_weights.argtypes = [C, W, c_int32, c_int32, P, P, c_int32, S, P, c_float, P, P, c_int64, c_int64, P]
+    lib.talon_paged_evict.argtypes = [C, C, P, c_int32, P, c_int64, c_int64, c_int32, c_int32, c_int32, P, P, P, c_int64, c_int64, P]
+    lib.talon_paged_compact.argtypes = [C, c_int32, P, P, P, P, P, c_int32, c_int64, c_int64, P]
     for name in EXPORTS:
         fn = getattr(lib, name)
         if fn.restype is c_int:
@@ -418,3 +446,77 @@ def talon_compact_kv(k_tree, v_tree, path, accept_len, prefix_len, new_prefix_le
 
 def talon_prune_tree(st: TreeState, n_keep: int, kept_ids, stream=None):
     _check(load_library().talon_prune_tree(_byref(st.c), n_keep, _ptr(kept_ids), _stream(stream)))
+
+
+class PagedCache:
+    """The pools and the page table of a cache kept in pages, plus the C struct that names them.
+
+    k, v: [pages][page_size][Hkv][Dh] bf16 or fp16 views that share strides (Dh contiguous; the tokens or the heads of a page
+    together); page_table int32 [B][max_pages], contiguous; status int32 [B], made here if it is not given, collects
+    TALON_STATUS_BAD_PAGE."""
+
+    def __init__(self, k: torch.Tensor, v: torch.Tensor, page_table: torch.Tensor, status: torch.Tensor | None = None):
+        if k.dim() != 4 or k.shape != v.shape or k.dtype != v.dtype or k.stride() != v.stride() or k.stride(3) != 1:
+            raise TalonError(TALON_ERR_INVALID_ARG, "k and v must be [pages][page_size][Hkv][Dh], of one type and one set of strides, Dh contiguous")
+        if k.dtype not in (torch.bfloat16, torch.float16):
+            raise TalonError(TALON_ERR_UNSUPPORTED, "cache dtype %s (bfloat16 or float16)" % k.dtype)
+        if page_table.dim() != 2 or page_table.dtype != torch.int32 or not page_table.is_contiguous():
+            raise TalonError(TALON_ERR_INVALID_ARG, "page_table must be contiguous int32 [B][max_pages]")
+        B = page_table.shape[0]
+        if status is None:
+            status = torch.zeros(B, dtype=torch.int32, device=page_table.device)
+        if status.shape != (B,) or status.dtype != torch.int32 or not status.is_contiguous():
+            raise TalonError(TALON_ERR_INVALID_ARG, "status must be contiguous int32 [B]")
+        if not (k.device == v.device == page_table.device == status.device):
+            raise TalonError(TALON_ERR_INVALID_ARG, "k, v, page_table and status must be on one device")
+        self.k, self.v, self.page_table, self.status = k, v, page_table, status
+        self.c = _CPagedCache(B, k.shape[2], k.shape[3], TALON_DTYPE_F16 if k.dtype == torch.float16 else TALON_DTYPE_BF16, k.shape[0],
+                              k.shape[1], page_table.shape[1], k.stride(0), k.stride(1), k.stride(2), k.data_ptr(), v.data_ptr(),
+                              page_table.data_ptr(), status.data_ptr())
+
+    def get_device(self) -> int:
+        return self.k.get_device()
+
+
+def talon_rotary_store(cache: PagedCache, q, k, v, q_out, n_new, prefix_len, pos, inv_freq, pos_base=None, pair_axis=None,
+                       interleaved=False, stream=None):
+    """q, q_out [B][N][Hq][Dh], k, v [B][N][Hkv][Dh] views with contiguous heads (parts of one fused tensor are fine, q_out may
+    be q); pos int32 [axes][B][N]; inv_freq float32 [pairs] (None: nothing is rotated); pos_base int32 [B], pair_axis int32
+    [pairs]."""
+    _native.rotary_store(cache, q, k, v, q_out, n_new, prefix_len, pos, inv_freq, pos_base, pair_axis, interleaved, stream)
+
+
+def talon_paged_attention_workspace_bytes(B, N, Hq, Hkv, Dh, max_prefix_len) -> int:
+    nb = load_library().talon_paged_attention_workspace_bytes(B, N, Hq, Hkv, Dh, max_prefix_len)
+    if nb == 0:
+        raise TalonError(TALON_ERR_INVALID_ARG, load_library().talon_last_error_string().decode())
+    return nb
+
+
+def talon_paged_attention(cache: PagedCache, q, n_new, prefix_len, max_prefix_len, out, out_lse=None, workspace=None, mask=None,
+                          offset=None, scale=0.0, softcap=0.0, slopes=None, window=0, stream=None):
+    """q, out [B][N][Hq][Dh] views with contiguous heads; out_lse float32 [B][N][Hq]; mask int64 [B][N][ceil(N/64)] (None:
+    causal) and offset int32 [B][N], e.g. a tree's mask and TreeState.depth; slopes float32 [Hq]."""
+    _native.paged_attention(cache, q, n_new, prefix_len, max_prefix_len, out, out_lse, workspace, mask, offset, scale, softcap, slopes,
+                            window, stream)
+
+
+def talon_paged_weights(cache: PagedCache, q, n_new, prefix_len, max_prefix_len, lse, weights, decay=1.0, prior=None, mask=None,
+                        offset=None, scale=0.0, softcap=0.0, slopes=None, window=0, stream=None):
+    """weights, prior float32 [B][Hkv][rows] with contiguous rows and one set of strides (prior may be weights; None: 0); the
+    other arguments as in talon_paged_attention, whose out_lse is `lse`."""
+    _native.paged_weights(cache, q, n_new, prefix_len, max_prefix_len, lse, weights, decay, prior, mask, offset, scale, softcap, slopes,
+                          window, stream)
+
+
+def talon_paged_evict(cache: PagedCache, length, max_len, weights, budget, kept, new_length, n_sink=0, n_recent=0, dst=None,
+                      new_weights=None, stream=None):
+    """weights, new_weights float32 [B][Hkv][rows]; kept int32 [B][Hkv][budget]; dst: a PagedCache of other pages (None: in
+    place)."""
+    _native.paged_evict(cache, length, max_len, weights, budget, kept, new_length, n_sink, n_recent, dst, new_weights, stream)
+
+
+def talon_paged_compact(cache: PagedCache, path, accept_len, prefix_len, new_prefix_len, weights=None, stream=None):
+    """path int32 [B][N] and accept_len as talon_greedy_accept writes them; weights float32 [B][Hkv][rows] move along (rows
+    that they do not have stay where they are)."""
+    _native.paged_compact(cache, path, accept_len, prefix_len, new_prefix_len, weights, stream)

@@ -15,7 +15,8 @@ LIB_PATH = os.path.join(LIB_DIR, "libtalon.so")
 MARSHAL_PATH = os.path.join(LIB_DIR, "_talon_marshal.so")
 OBJ_DIR = os.path.join(PKG, "_build")
 
-SOURCES = ["api.hip", "expand.hip", "ahead.hip", "select.hip", "literal.hip", "attention.hip", "accept.hip", "calibrate.hip"]
+SOURCES = ["api.hip", "expand.hip", "ahead.hip", "select.hip", "literal.hip", "attention.hip", "accept.hip", "calibrate.hip",
+           "paged_api.hip", "paged_attention_bf16.hip", "paged_attention_f16.hip", "paged_weights.hip", "paged_rows.hip"]
 
 FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
@@ -49,7 +50,7 @@ def build(verbose: bool = False) -> str:
     def compile_one(i):
         return _run([hipcc, *FLAGS, "-c", os.path.join(CSRC, SOURCES[i]), "-o", objs[i]])
 
-    with ThreadPoolExecutor(max_workers=6) as ex:
+    with ThreadPoolExecutor(max_workers=8) as ex:
         for out in ex.map(compile_one, range(len(SOURCES))):
             if verbose and out.strip():
                 print(out)

@@ -8,6 +8,7 @@
 #include <Python.h>
 
 #include <stdint.h>
+#include <stdio.h>
 #include <string.h>
 
 #include "talon.h"
@@ -32,6 +33,11 @@ struct Abi {
   decltype(&talon_build_tree_mask) build_tree_mask;
   decltype(&talon_tree_attention) tree_attention;
   decltype(&talon_tree_attention_static) tree_attention_static;
+  decltype(&talon_rotary_store) rotary_store;
+  decltype(&talon_paged_attention) paged_attention;
+  decltype(&talon_paged_weights) paged_weights;
+  decltype(&talon_paged_evict) paged_evict;
+  decltype(&talon_paged_compact) paged_compact;
 };
 constexpr int kFunctions = sizeof(Abi) / sizeof(void*);
 Abi g_abi;   // (set under the interpreter lock)
@@ -41,7 +47,9 @@ PyObject *g_error, *g_float32, *g_bfloat16, *g_int_of, *g_float_of, *g_stream_of
     *g_initialized;   // (the last three may be None)
 // ---- interned names
 PyObject *n_data_ptr, *n_stride, *n_shape, *n_dtype, *n_nbytes, *n_token, *n_logit, *n_prob, *n_edge_logp, *n_row_max, *n_row_lse,
-    *n_is_contiguous, *n_numel;
+    *n_is_contiguous, *n_numel, *n_get_device, *n_c;
+// ---- the types of the tensors that the calls on a paged cache take
+PyObject *g_float16, *g_int32, *g_int64;
 
 // One call: the first failure is kept (Python's error indicator is set), later steps do nothing.
 struct Call {
@@ -477,6 +485,279 @@ PyObject* tree_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return result(c, rc);
 }
 
+// ---- calls on a paged cache.  Their tensors are checked here: type, shape, strides, and that all lie on the current device
+// (a host pointer or another device's would only be noticed by the GPU).
+struct Paged {
+  Call& c;
+  Py_buffer buffer = {};
+  bool have_buffer = false, second_have = false;
+  Py_buffer second = {};
+  const talon_paged_cache* cache = nullptr;
+  const char* astray = nullptr;   // a tensor that is not on the current device
+  long long device = -1;
+  PyObject* storage = nullptr;    // the cache's torch dtype (borrowed)
+
+  explicit Paged(Call& call) : c(call) {}
+  ~Paged() {
+    if (have_buffer) PyBuffer_Release(&buffer);
+    if (second_have) PyBuffer_Release(&second);
+  }
+  void invalid(const char* name, const char* what) {
+    if (!c.ok) return;
+    char text[200];
+    snprintf(text, sizeof text, "%s %s", name, what);
+    c.refuse(TALON_ERR_INVALID_ARG, text);
+  }
+  const talon_paged_cache* struct_of(PyObject* o, Py_buffer* to, bool* have) {   // binding.PagedCache
+    PyObject* s = c.attr(o, n_c);
+    const talon_paged_cache* r = nullptr;
+    if (s) {
+      if (PyObject_GetBuffer(s, to, PyBUF_SIMPLE) != 0) c.fail();
+      else {
+        *have = true;
+        if (to->len != static_cast<Py_ssize_t>(sizeof(talon_paged_cache))) {
+          PyErr_SetString(PyExc_TypeError, "a PagedCache is required");
+          c.fail();
+        } else r = static_cast<const talon_paged_cache*>(to->buf);
+      }
+      Py_DECREF(s);
+    }
+    place(o, "the cache");
+    return r;
+  }
+  bool open(PyObject* o) {
+    cache = struct_of(o, &buffer, &have_buffer);
+    if (cache) storage = cache->dtype == TALON_DTYPE_F16 ? g_float16 : g_bfloat16;
+    return cache != nullptr;
+  }
+  const talon_paged_cache* other(PyObject* o) { return struct_of(o, &second, &second_have); }
+  void place(PyObject* t, const char* name) {
+    PyObject* d = c.call(t, n_get_device);
+    const long long at = c.steal_i64(d);
+    if (!c.ok || astray) return;
+    if (device < 0 && at >= 0 && g_device != Py_None) device = c.steal_i64(PyObject_CallNoArgs(g_device));
+    if (at < 0 || (device >= 0 && at != device)) astray = name;
+  }
+  // Checks type and dimensions; dims[i] >= 0 is asked for, -1 is filled in.  strides: of all dimensions.
+  void* tensor(PyObject* t, PyObject* type, int n, int64_t* dims, int64_t* strides, const char* name, PyObject* type2 = nullptr) {
+    if (!c.ok) return nullptr;
+    if (t == Py_None) { invalid(name, "is None"); return nullptr; }
+    PyObject* dt = c.attr(t, n_dtype);
+    if (dt && dt != type && dt != type2) {
+      PyObject* text = PyUnicode_FromFormat("%s must be %S, not %S", name, type, dt);
+      if (text) { c.refuse(TALON_ERR_INVALID_ARG, PyUnicode_AsUTF8(text)); Py_DECREF(text); } else c.fail();
+    }
+    Py_XDECREF(dt);
+    const char* shape_text = "has another shape than the call needs";
+    PyObject* shape = c.attr(t, n_shape);
+    if (shape) {
+      if (!PyTuple_Check(shape) || PyTuple_GET_SIZE(shape) != n) invalid(name, shape_text);
+      for (int i = 0; c.ok && i < n; ++i) {
+        const int64_t d = c.item(shape, i);
+        if (dims[i] >= 0 && d != dims[i]) invalid(name, shape_text);
+        dims[i] = d;
+        if (d > 0x7FFFFFFF) invalid(name, shape_text);
+      }
+      Py_DECREF(shape);
+    }
+    PyObject* st = c.call(t, n_stride);
+    if (st) {
+      for (int i = 0; c.ok && i < n; ++i) strides[i] = c.item(st, i);
+      Py_DECREF(st);
+    }
+    place(t, name);
+    return c.ptr(t);
+  }
+  void* dense(PyObject* t, PyObject* type, int n, int64_t* dims, const char* name, PyObject* type2 = nullptr) {
+    int64_t strides[4] = {0, 0, 0, 0};
+    void* p = tensor(t, type, n, dims, strides, name, type2);
+    int64_t want = 1;
+    for (int i = n - 1; c.ok && i >= 0; --i) {
+      if (dims[i] != 1 && strides[i] != want) invalid(name, "must be contiguous");
+      want *= dims[i];
+    }
+    return p;
+  }
+  const int32_t* per_sequence(PyObject* t, const char* name) {
+    int64_t d[1] = {cache ? cache->B : -1};
+    return static_cast<const int32_t*>(dense(t, g_int32, 1, d, name));
+  }
+  // [B][N][H][Dh]; N and H are asked for or filled in
+  talon_view view(PyObject* t, int64_t* N, int64_t* H, const char* name) {
+    talon_view v = {};
+    int64_t d[4] = {cache ? cache->B : -1, *N, *H, cache ? cache->Dh : -1}, s[4] = {0, 0, 0, 0};
+    v.data = tensor(t, storage, 4, d, s, name);
+    if (c.ok && d[3] != 1 && s[3] != 1) invalid(name, "must have contiguous heads");
+    v.stride_b = s[0]; v.stride_t = s[1]; v.stride_h = s[2];
+    *N = d[1];
+    *H = d[2];
+    return v;
+  }
+  // [B][Hkv][rows] in fp32 with contiguous rows, `least` of them
+  float* rows(PyObject* t, int64_t least, int64_t* sb, int64_t* sh, const char* name, int64_t* count = nullptr) {
+    int64_t d[3] = {cache ? cache->B : -1, cache ? cache->Hkv : -1, -1}, s[3] = {0, 0, 0};
+    float* p = static_cast<float*>(tensor(t, g_float32, 3, d, s, name));
+    if (c.ok && d[2] != 1 && s[2] != 1) invalid(name, "must have contiguous rows");
+    if (c.ok && d[2] < least) invalid(name, "has fewer rows than the call may touch");
+    if (count) *count = d[2];
+    *sb = d[0] == 1 ? d[2] : s[0];
+    *sh = d[1] == 1 ? d[2] : s[1];
+    return p;
+  }
+  int64_t capacity() const { return cache ? static_cast<int64_t>(cache->max_pages) * cache->page_size : 0; }
+  // mask, offset, scale, softcap, slopes, window
+  talon_scores scores(PyObject* const* a, int64_t N, int64_t Hq) {
+    talon_scores s = {};
+    const int64_t B = cache ? cache->B : -1;
+    if (a[0] != Py_None) {
+      int64_t d[3] = {B, N, (N + 63) / 64};
+      s.mask = static_cast<const uint64_t*>(dense(a[0], g_int64, 3, d, "mask"));
+    }
+    if (a[1] != Py_None) {
+      int64_t d[2] = {B, N};
+      s.offset = static_cast<const int32_t*>(dense(a[1], g_int32, 2, d, "offset"));
+    }
+    s.scale = c.f32(a[2]);
+    s.softcap = c.f32(a[3]);
+    if (a[4] != Py_None) {
+      int64_t d[1] = {Hq};
+      s.slopes = static_cast<const float*>(dense(a[4], g_float32, 1, d, "slopes"));
+    }
+    s.window = c.i32(a[5]);
+    return s;
+  }
+  // the last check in front of a call
+  void on_device() {
+    if (c.ok && astray) invalid(astray, "is not on the current GPU");
+  }
+};
+
+// (cache, q, k, v, q_out, n_new, prefix_len, pos, inv_freq, pos_base, pair_axis, interleaved, stream)
+PyObject* rotary_store(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  if (!arguments(n, 13)) return nullptr;
+  Call c;
+  Paged p(c);
+  p.open(a[0]);
+  int64_t N = -1, Hq = -1, Hkv = p.cache ? p.cache->Hkv : -1;
+  const talon_view q = p.view(a[1], &N, &Hq, "q"), k = p.view(a[2], &N, &Hkv, "k"), v = p.view(a[3], &N, &Hkv, "v"),
+                   out = p.view(a[4], &N, &Hq, "q_out");
+  const int32_t *fresh = p.per_sequence(a[5], "n_new"), *prefix = p.per_sequence(a[6], "prefix_len");
+  int64_t d3[3] = {-1, p.cache ? p.cache->B : -1, N}, pairs[1] = {0};
+  const float* freq = nullptr;
+  const int32_t *pos = nullptr, *base = nullptr, *axis = nullptr;
+  if (a[8] != Py_None) {
+    pairs[0] = -1;
+    freq = static_cast<const float*>(p.dense(a[8], g_float32, 1, pairs, "inv_freq"));
+  }
+  if (a[7] != Py_None) pos = static_cast<const int32_t*>(p.dense(a[7], g_int32, 3, d3, "pos"));
+  else d3[0] = 1;
+  if (a[9] != Py_None) base = p.per_sequence(a[9], "pos_base");
+  if (a[10] != Py_None) axis = static_cast<const int32_t*>(p.dense(a[10], g_int32, 1, pairs, "pair_axis"));
+  const int interleaved = PyObject_IsTrue(a[11]);
+  if (interleaved < 0) c.fail();
+  p.on_device();
+  void* s = c.stream(a[12]);
+  RUN(rc, g_abi.rotary_store(p.cache, &q, &k, &v, &out, static_cast<int32_t>(N), static_cast<int32_t>(Hq), fresh, prefix, pos,
+                             static_cast<int32_t>(d3[0]), base, freq, static_cast<int32_t>(pairs[0]), axis, interleaved, s))
+  return result(c, rc);
+}
+
+// (cache, q, n_new, prefix_len, max_prefix_len, out, out_lse, workspace, mask, offset, scale, softcap, slopes, window, stream)
+PyObject* paged_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  if (!arguments(n, 15)) return nullptr;
+  Call c;
+  Paged p(c);
+  p.open(a[0]);
+  int64_t N = -1, Hq = -1;
+  const talon_view q = p.view(a[1], &N, &Hq, "q");
+  const int32_t *fresh = p.per_sequence(a[2], "n_new"), *prefix = p.per_sequence(a[3], "prefix_len");
+  const int32_t most = c.i32(a[4]);
+  const talon_view out = p.view(a[5], &N, &Hq, "out");
+  float* lse = nullptr;
+  if (a[6] != Py_None) {
+    int64_t d[3] = {p.cache ? p.cache->B : -1, N, Hq};
+    lse = static_cast<float*>(p.dense(a[6], g_float32, 3, d, "out_lse"));
+  }
+  void* ws = c.ptr(a[7]);
+  const size_t bytes = a[7] == Py_None ? 0 : c.nbytes(a[7]);
+  if (a[7] != Py_None) p.place(a[7], "workspace");
+  const talon_scores sc = p.scores(a + 8, N, Hq);
+  p.on_device();
+  void* s = c.stream(a[14]);
+  RUN(rc, g_abi.paged_attention(p.cache, &q, static_cast<int32_t>(N), static_cast<int32_t>(Hq), fresh, prefix, most, &sc, &out, lse, ws, bytes, s))
+  return result(c, rc);
+}
+
+// (cache, q, n_new, prefix_len, max_prefix_len, lse, weights, decay, prior, mask, offset, scale, softcap, slopes, window, stream)
+PyObject* paged_weights(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  if (!arguments(n, 16)) return nullptr;
+  Call c;
+  Paged p(c);
+  p.open(a[0]);
+  int64_t N = -1, Hq = -1;
+  const talon_view q = p.view(a[1], &N, &Hq, "q");
+  const int32_t *fresh = p.per_sequence(a[2], "n_new"), *prefix = p.per_sequence(a[3], "prefix_len");
+  const int32_t most = c.i32(a[4]);
+  int64_t d[3] = {p.cache ? p.cache->B : -1, N, Hq};
+  const float* lse = static_cast<const float*>(p.dense(a[5], g_float32, 3, d, "lse"));
+  const int64_t touched = most + N < p.capacity() ? most + N : p.capacity();
+  int64_t sb = 0, sh = 0, pb = 0, ph = 0;
+  float* w = p.rows(a[6], touched, &sb, &sh, "weights");
+  const float decay = c.f32(a[7]);
+  const float* prior = nullptr;
+  if (a[8] != Py_None) {
+    prior = p.rows(a[8], most < touched ? most : touched, &pb, &ph, "prior");
+    if ((p.cache && p.cache->B > 1 && pb != sb) || (p.cache && p.cache->Hkv > 1 && ph != sh)) p.invalid("prior", "must have the strides of weights");
+  }
+  const talon_scores sc = p.scores(a + 9, N, Hq);
+  p.on_device();
+  void* s = c.stream(a[15]);
+  RUN(rc, g_abi.paged_weights(p.cache, &q, static_cast<int32_t>(N), static_cast<int32_t>(Hq), fresh, prefix, most, &sc, lse, decay, prior, w, sb, sh, s))
+  return result(c, rc);
+}
+
+// (cache, length, max_len, weights, budget, kept, new_length, n_sink, n_recent, dst, new_weights, stream)
+PyObject* paged_evict(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  if (!arguments(n, 12)) return nullptr;
+  Call c;
+  Paged p(c);
+  p.open(a[0]);
+  const int32_t* len = p.per_sequence(a[1], "length");
+  const int32_t most = c.i32(a[2]);
+  const int64_t touched = most < p.capacity() ? most : p.capacity();
+  int64_t sb = 0, sh = 0, nb = 0, nh = 0;
+  const float* w = p.rows(a[3], touched, &sb, &sh, "weights");
+  const int32_t budget = c.i32(a[4]);
+  int64_t d[3] = {p.cache ? p.cache->B : -1, p.cache ? p.cache->Hkv : -1, budget < 0 ? 0 : budget};
+  int32_t* kept = static_cast<int32_t*>(p.dense(a[5], g_int32, 3, d, "kept"));
+  int32_t* new_len = const_cast<int32_t*>(p.per_sequence(a[6], "new_length"));
+  const int32_t sink = c.i32(a[7]), recent = c.i32(a[8]);
+  const talon_paged_cache* dst = a[9] == Py_None ? nullptr : p.other(a[9]);
+  float* new_w = a[10] == Py_None ? nullptr : p.rows(a[10], budget < touched ? budget : touched, &nb, &nh, "new_weights");
+  p.on_device();
+  void* s = c.stream(a[11]);
+  RUN(rc, g_abi.paged_evict(p.cache, dst, len, most, w, sb, sh, budget, sink, recent, kept, new_len, new_w, nb, nh, s))
+  return result(c, rc);
+}
+
+// (cache, path, accept_len, prefix_len, new_prefix_len, weights, stream)
+PyObject* paged_compact(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  if (!arguments(n, 7)) return nullptr;
+  Call c;
+  Paged p(c);
+  p.open(a[0]);
+  int64_t d[2] = {p.cache ? p.cache->B : -1, -1};
+  const int32_t* path = static_cast<const int32_t*>(p.dense(a[1], g_int32, 2, d, "path"));
+  const int32_t *len = p.per_sequence(a[2], "accept_len"), *prefix = p.per_sequence(a[3], "prefix_len");
+  int32_t* new_prefix = const_cast<int32_t*>(p.per_sequence(a[4], "new_prefix_len"));
+  int64_t sb = 0, sh = 0, rows = 0;
+  float* w = a[5] == Py_None ? nullptr : p.rows(a[5], 0, &sb, &sh, "weights", &rows);
+  p.on_device();
+  void* s = c.stream(a[6]);
+  RUN(rc, g_abi.paged_compact(p.cache, static_cast<int32_t>(d[1]), path, len, prefix, new_prefix, w, static_cast<int32_t>(rows), sb, sh, s))
+  return result(c, rc);
+}
+
 // (addresses of the functions in the order of Abi, TalonError, torch.float32, torch.bfloat16, binding._int_of and _float_of,
 // binding._stream and what it asks: raw handle of a device's current stream, current device, is the GPU initialised)
 PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
@@ -501,6 +782,16 @@ PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
     Py_XDECREF(*keep[i]);
     *keep[i] = a[1 + i];
   }
+  PyObject* torch = PyImport_ImportModule("torch");
+  if (!torch) return nullptr;
+  struct { PyObject** at; const char* name; } const types[] = {{&g_float16, "float16"}, {&g_int32, "int32"}, {&g_int64, "int64"}};
+  for (const auto& t : types) {
+    PyObject* found = PyObject_GetAttrString(torch, t.name);
+    if (!found) { Py_DECREF(torch); return nullptr; }
+    Py_XDECREF(*t.at);
+    *t.at = found;
+  }
+  Py_DECREF(torch);
   Py_RETURN_NONE;
 }
 
@@ -511,6 +802,8 @@ PyMethodDef g_methods[] = {METHOD(bind, bind), METHOD(tree_init, tree_init), MET
                            METHOD(expand_literal, expand_literal), METHOD(target_argmax, target_argmax),
                            METHOD(greedy_accept, greedy_accept), METHOD(compact_kv, compact_kv),
                            METHOD(build_tree_mask, build_tree_mask), METHOD(tree_attention, tree_attention),
+                           METHOD(rotary_store, rotary_store), METHOD(paged_attention, paged_attention),
+                           METHOD(paged_weights, paged_weights), METHOD(paged_evict, paged_evict), METHOD(paged_compact, paged_compact),
                            {nullptr, nullptr, 0, nullptr}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_talon_marshal", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};
 
@@ -520,7 +813,8 @@ PyMODINIT_FUNC PyInit__talon_marshal(void) {
   struct { PyObject** at; const char* text; } const names[] = {
       {&n_data_ptr, "data_ptr"}, {&n_stride, "stride"}, {&n_shape, "shape"}, {&n_dtype, "dtype"}, {&n_nbytes, "nbytes"},
       {&n_token, "token"}, {&n_logit, "logit"}, {&n_prob, "prob"}, {&n_edge_logp, "edge_logp"}, {&n_row_max, "row_max"},
-      {&n_row_lse, "row_lse"}, {&n_is_contiguous, "is_contiguous"}, {&n_numel, "numel"}};
+      {&n_row_lse, "row_lse"}, {&n_is_contiguous, "is_contiguous"}, {&n_numel, "numel"},
+      {&n_get_device, "get_device"}, {&n_c, "c"}};
   for (const auto& n : names)
     if (!(*n.at = PyUnicode_InternFromString(n.text))) return nullptr;
   return PyModule_Create(&g_module);

@@ -1,0 +1,782 @@
+// Attention of new tokens over a paged cache (App. B's tree attention where the cache is kept in pages), included by one
+// source per storage type.
+//
+//   x_ij = scale q_i . k_j,   capped: cap tanh(x / cap),   biased: - slope_h |p_i - p_j|,   -inf where i does not see j
+//   out_i = sum_j softmax_j(x_ij) v_j,   lse_i = log sum_j exp(x_ij)
+//
+// One pass over the rows of K and V: running maximum, denominator and output (fp32).  The rows of the new tokens lie in the
+// cache like all others, so there is one kind of key tile.
+//
+// Tiling.  The G query heads of a KV head and the new tokens make one row dimension (row = token * G + head).  A workgroup of
+// NW = 4 or 8 wavefronts takes 32 * NW of these rows, 32 a wavefront, and streams 64-row tiles of K and V through LDS (two
+// stages each, global to LDS without registers).  Both products are formed transposed (a query is a lane):
+//   S^T[key][query] = K . Q^T,   O^T[dh][query] += V^T . P^T
+// so that the accumulators of S^T are the operand P^T of the second product as they stand, and the statistics of a row are
+// scalars of a lane.  While the matrix pipe forms the scores of tile t + 1 the vector pipe takes the exponentials of tile t.
+//
+// Work.  Every (sequence, KV head, row tile) needs a number of key tiles that the host does not know (lengths are on the
+// device).  All of them, end to end in that order, are one line of W tiles, cut into equal shares of ceil(W / workgroups), at
+// least `least`: whatever the lengths are, no workgroup has more than a tile more than another.  A share ends inside a row
+// tile as a rule: what it has of it goes to a slot (output not yet divided, maximum, denominator; fp32), and a second kernel
+// joins the slots of a row tile in the order of the shares.  A row tile that lies in one share is written at once.
+// A share's first incomplete piece lies in slot 2 * share, a last one that is not also its first in 2 * share + 1; cut[share]
+// says what the merge behind the share's end has to do: {sequence * Hkv + KV head, first row, rows, last share | (slot & 1) << 30},
+// rows = 0 where nothing begins to be cut there.  Where every row tile has a few key tiles at most, nothing is cut: a share is
+// a row tile, and there is no second launch.
+//
+// Values of V that are no finite numbers must not reach a row that does not see them (0 * NaN), so a tile that some row of the
+// workgroup does not see whole is looked through for them first; where there are any they are set to zero and the rows that
+// do see them become NaN.
+#pragma once
+
+#include <type_traits>
+
+#include "paged_device.h"
+
+namespace talon {
+
+namespace {
+
+typedef float floatx16 __attribute__((ext_vector_type(16)));
+typedef short short4v __attribute__((ext_vector_type(4)));
+typedef short short8v __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+template <bool F16>
+struct Storage {
+  using x8 = std::conditional_t<F16, f16x8, bf16x8>;
+  using x4 = std::conditional_t<F16, f16x4, bf16x4>;
+  using x1 = std::conditional_t<F16, _Float16, __bf16>;
+  static constexpr uint32_t kExponents = F16 ? 0x7C007C00u : 0x7F807F80u;   // of two values
+  static __device__ __forceinline__ floatx16 mfma(x8 a, x8 b, floatx16 c) {
+    if constexpr (F16) return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
+    else return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+  }
+  // bit 0: the lower of the two values is no finite number, bit 1: the upper one
+  static __device__ __forceinline__ uint32_t not_finite(uint32_t two) {
+    const uint32_t e = two & kExponents;
+    return ((e & 0xFFFFu) == (kExponents & 0xFFFFu) ? 1u : 0u) | ((e >> 16) == (kExponents >> 16) ? 2u : 0u);
+  }
+};
+
+constexpr int kTileRows = 64;
+
+// 16 bytes per lane from global memory to LDS, lane l at lds_base + 16 * l.  In assembly, because the compiler waits for all
+// outstanding loads of its builtin before any LDS read; the waits are tile_landed()'s.
+__device__ __forceinline__ void global_to_lds(const uint16_t* src, const uint16_t* lds_base) {
+  const uint32_t lds_addr = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(
+      (__attribute__((address_space(3))) void*)(lds_base)));
+  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off"
+               :: "v"(src), "s"(lds_addr) : "memory", "m0");
+}
+
+// LDS image of a tile: rows of DH values without padding, the 16-byte chunks of a row permuted (differently for K, read as
+// 16-byte fragments of 16 rows, and V, read by the transposing load) so that no two lanes of a read share a bank.
+template <int DH>
+struct PagedSmem {
+  static constexpr int CPR = DH / 8;
+  static constexpr int T_ELEMS = kTileRows * DH;
+  static constexpr int POS_BYTES = 8 * kTileRows * 4;              // positions of a tile's rows, one copy per wavefront
+  static constexpr int BYTES = 4 * T_ELEMS * 2 + POS_BYTES + 16;   // two stages of K, two of V; the rows of V that are not finite
+  __device__ static int kswz(int row) { return DH >= 128 ? (row & 15) : ((row >> 1) & 7); }
+  __device__ static int vswz(int row) { return DH >= 128 ? ((row & 3) << 2) : (((row >> 1) & 1) << 2); }
+};
+
+// Key tiles [*first, *first + result) of row tile rt of a sequence.
+__device__ __forceinline__ int tiles_of(const ScoreArgs& sc, int P, int n, uint32_t inv_g, int row_tile, int rt, int* first) {
+  int last = div_g((rt + 1) * row_tile - 1, inv_g);
+  last = last < n - 1 ? last : n - 1;
+  const int end = sc.mask != nullptr ? P + n : P + last + 1;
+  int begin = 0;
+  if (sc.window > 0) {
+    const int lowest = P + (sc.offset != nullptr || sc.mask != nullptr ? 0 : div_g(rt * row_tile, inv_g));
+    begin = lowest - sc.window + 1;
+    begin = begin < 0 ? 0 : begin;
+  }
+  *first = begin / kTileRows;
+  return (end + kTileRows - 1) / kTileRows - begin / kTileRows;
+}
+
+template <bool F16, int DH, int NW, bool MOD>
+__global__ __launch_bounds__(64 * NW, DH == 256 ? 1 : (NW == 4 ? 2 : 1)) void paged_attention_kernel(PagedAttnArgs a) {
+  using ST = Storage<F16>;
+  using x8 = typename ST::x8;
+  using x4 = typename ST::x4;
+  using SM = PagedSmem<DH>;
+  constexpr int kWgThreads = 64 * NW;
+  constexpr int DSTEPS = DH / 16;
+  constexpr int DB = DH / 32;
+  constexpr int CPR = DH / 8;
+  constexpr int kRowTile = 32 * NW;
+  extern __shared__ __attribute__((aligned(16))) uint16_t smem[];
+
+  const int tid = threadIdx.x;
+  const int lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int l32 = lane & 31;
+  const int h = lane >> 5;
+  const ScoreArgs& sc = a.sc;
+  const int G = a.G;
+
+  // ---- this workgroup's share.  Workgroup ids are dealt round-robin to the 8 XCDs: neighbouring shares, which read the same
+  // rows of K and V where a sequence has several row tiles, go to one XCD and its L2.
+  const int per_xcd = (static_cast<int>(gridDim.x) + 7) / 8;
+  const int share = static_cast<int>(blockIdx.x % 8) * per_xcd + static_cast<int>(blockIdx.x / 8);   // (the grid is a multiple of 8)
+  const bool split = a.cut != nullptr;   // else a share is a row tile
+  int b = 0, g = 0, rt = 0, at = 0, x_end = 0, x = 0, P = 0, n = 0, share_tiles = 0;
+  {
+    // lane l: sequences l, l + 64, ...
+    int sum_l[TALON_B_MAX / 64], P_l[TALON_B_MAX / 64], n_l[TALON_B_MAX / 64];
+    int total_l = 0;
+#pragma unroll
+    for (int c = 0; c < TALON_B_MAX / 64; ++c) {
+      sum_l[c] = P_l[c] = n_l[c] = 0;
+      if (c * 64 < a.B) {
+        const int bb = c * 64 + lane;
+        if (bb < a.B) {
+          clamped_lengths(a.c, sc.prefix_len[bb], sc.n_new[bb], sc.max_prefix_len, sc.N, &P_l[c], &n_l[c]);
+          const int row_tiles = (n_l[c] * G + kRowTile - 1) / kRowTile;
+          int first;
+          if (!split) sum_l[c] = row_tiles;
+          else for (int r = 0; r < row_tiles; ++r) sum_l[c] += tiles_of(sc, P_l[c], n_l[c], a.inv_g, kRowTile, r, &first);
+          sum_l[c] *= a.Hkv;
+          total_l += sum_l[c];
+        }
+      }
+    }
+    const int total = __builtin_amdgcn_readfirstlane(wave_sum_i32(total_l));
+    share_tiles = (total + a.slots - 1) / a.slots;
+    share_tiles = share_tiles < a.least ? a.least : share_tiles;
+    const long long x0 = static_cast<long long>(share) * share_tiles;
+    if (x0 >= total) {
+      if (split && tid == 0 && share < a.slots) a.cut[share] = make_int4(0, 0, 0, 0);
+      return;
+    }
+    x = static_cast<int>(x0);
+    x_end = total - x < share_tiles ? total : x + share_tiles;
+    int before = 0;
+#pragma unroll
+    for (int c = 0; c < TALON_B_MAX / 64; ++c) {
+      if (c * 64 < a.B) {
+        const int incl = wave_inclusive_scan_i32(sum_l[c]);
+        const int begin = before + incl - sum_l[c];
+        before += __builtin_amdgcn_readlane(incl, 63);
+        const unsigned long long in = __ballot(x >= begin && x < begin + sum_l[c]);
+        if (in != 0ull) {
+          const int l = __ffsll(static_cast<long long>(in)) - 1;
+          b = c * 64 + l;
+          at = x - __builtin_amdgcn_readlane(begin, l);
+          P = __builtin_amdgcn_readlane(P_l[c], l);
+          n = __builtin_amdgcn_readlane(n_l[c], l);
+          const int per_head = __builtin_amdgcn_readlane(sum_l[c], l) / a.Hkv;
+          g = at / per_head;
+          at -= g * per_head;
+        }
+      }
+    }
+    if (!split) {
+      rt = at;
+      at = 0;
+    }
+    for (int first; split; ++rt) {
+      const int t = tiles_of(sc, P, n, a.inv_g, kRowTile, rt, &first);
+      if (at < t) break;
+      at -= t;
+    }
+  }
+  if (split && tid == 0) a.cut[share] = make_int4(0, 0, 0, 0);
+
+  const uint16_t* const k_pool = static_cast<const uint16_t*>(a.c.k);
+  const uint16_t* const v_pool = static_cast<const uint16_t*>(a.c.v);
+  int* const s_pos = reinterpret_cast<int*>(smem + 4 * SM::T_ELEMS) + wave * kTileRows;
+  uint32_t* const s_bad = reinterpret_cast<uint32_t*>(smem + 4 * SM::T_ELEMS) + SM::POS_BYTES / 4;
+  auto stage_k = [&](int st) { return smem + st * SM::T_ELEMS; };
+  auto stage_v = [&](int st) { return smem + (2 + st) * SM::T_ELEMS; };
+
+  // Tile loads.  With eight wavefronts the last four issue them: a compute unit's address path takes a tile pair's 32 KB in
+  // about 512 cycles whoever issues them, and a wavefront waits at its loads for its turn.
+  constexpr int ROWS_PER_LOAD = 64 / CPR;
+  constexpr int LW = NW == 8 ? 4 : NW;
+  constexpr int LOADS = kTileRows / ROWS_PER_LOAD / LW;
+  const int lwave = wave - (NW - LW);
+  const bool loader = lwave >= 0;
+  const int lrow = lane / CPR;
+  const int cslot = lane % CPR;
+
+  bool first_piece = true;
+  while (x < x_end) {
+    // ---- the piece: key tiles [t_begin, t_end) of (b, g, rt)
+    int first_tile;
+    const int tiles = tiles_of(sc, P, n, a.inv_g, kRowTile, rt, &first_tile);
+    const int take = !split || tiles - at < x_end - x ? tiles - at : x_end - x;
+    const int t_begin = first_tile + at;
+    const int nt = take;
+    const bool whole = take == tiles;
+    const int rows = n * G;
+    const int row0 = rt * kRowTile;
+    const int wrow0 = row0 + wave * 32;
+    const int tk0 = div_g(row0, a.inv_g);
+    int tk1 = div_g(row0 + kRowTile - 1, a.inv_g);
+    tk1 = tk1 < n - 1 ? tk1 : n - 1;
+    const int kend = sc.mask != nullptr ? P + n : P + tk1 + 1;   // rows of the cache that the tile looks at
+    const bool works = wrow0 < rows;                              // this wavefront has queries
+
+    // ---- this lane's query
+    const int rho = wrow0 + l32;
+    const bool valid = rho < rows;
+    const int token = valid ? div_g(rho, a.inv_g) : tk0;
+    const int head = g * G + (valid ? rho - token * G : 0);
+    const int off = offset_of(sc, b, token);
+    const int p_i = P + off;
+    float slope2 = 0.f;
+    if constexpr (MOD) if (sc.slopes != nullptr) slope2 = sc.slopes[head] * kLog2eF;
+
+    // ---- which tiles every row of the workgroup sees whole: those inside [seen_from, seen_to)
+    const bool positions = sc.window > 0 || (MOD && sc.slopes != nullptr);
+    int seen_to = sc.mask != nullptr || (positions && sc.offset != nullptr) ? P : P + tk0 + 1;
+    int seen_from = 0;
+    if (sc.window > 0) {
+      int most = tk1;
+      if (sc.offset != nullptr) {
+        most = 0;
+        for (int i = tk0 + lane; i <= tk1; i += 64) { const int o = offset_of(sc, b, i); most = most > o ? most : o; }
+        most = __builtin_amdgcn_readfirstlane(wave_max_i32(most));
+      }
+      seen_from = P + most - sc.window + 1;
+    }
+    auto partly_seen = [&](int t) { return (t + 1) * kTileRows > seen_to || t * kTileRows < seen_from; };
+
+    float m_run = kNoScore, l_run = 0.f;
+    floatx16 o[DB];
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) o[db][r] = 0.f;
+
+    // ---- addresses of a tile's rows.  A row past the end reads the last row instead; its score is masked.
+    uint32_t entry[LOADS], k_rows[LOADS], v_rows[LOADS];
+    auto key_of = [&](int t, int i) {
+      const int key = t * kTileRows + (lwave * LOADS + i) * ROWS_PER_LOAD + lrow;
+      return key < kend ? key : kend - 1;
+    };
+    auto load_entries = [&](int t) {
+      if (!loader) return;
+#pragma unroll
+      for (int i = 0; i < LOADS; ++i) entry[i] = page_entry(a.c, b, key_of(t, i));
+    };
+    // (waited for here, in front of the tile loads: where they were first used the wait would count those too)
+    auto entries_landed = [&]() {
+      static_assert(LOADS == 2 || LOADS == 4 || LOADS == 8, "one statement names every entry");
+      if constexpr (LOADS == 2) asm volatile("" : "+v"(entry[0]), "+v"(entry[1]));
+      else if constexpr (LOADS == 4) asm volatile("" : "+v"(entry[0]), "+v"(entry[1]), "+v"(entry[2]), "+v"(entry[3]));
+      else asm volatile("" : "+v"(entry[0]), "+v"(entry[1]), "+v"(entry[2]), "+v"(entry[3]), "+v"(entry[4]), "+v"(entry[5]), "+v"(entry[6]), "+v"(entry[7]));
+    };
+    auto rows_of = [&](int t, uint32_t (&to)[LOADS]) {
+      bool bad = false;
+#pragma unroll
+      for (int i = 0; i < LOADS; ++i) {
+        bad = bad || entry[i] >= a.c.num_pages;
+        to[i] = row_chunk(a.c, entry[i], key_of(t, i), g);
+      }
+      if (__ballot(bad) != 0ull && lane == 0) report(a.c, b, TALON_STATUS_BAD_PAGE);
+    };
+    auto load_k = [&](const uint32_t (&rows_)[LOADS], int st) {
+#pragma unroll
+      for (int i = 0; i < LOADS; ++i) {
+        const int u = (lwave * LOADS + i) * ROWS_PER_LOAD;
+        global_to_lds(chunk_at(k_pool, rows_[i] + (cslot ^ SM::kswz(u + lrow))), stage_k(st) + u * DH);
+      }
+    };
+    auto load_v = [&](const uint32_t (&rows_)[LOADS], int st) {
+#pragma unroll
+      for (int i = 0; i < LOADS; ++i) {
+        const int u = (lwave * LOADS + i) * ROWS_PER_LOAD;
+        global_to_lds(chunk_at(v_pool, rows_[i] + (cslot ^ SM::vswz(u + lrow))), stage_v(st) + u * DH);
+      }
+    };
+    auto tile_landed = [&]() {
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+      __syncthreads();
+    };
+
+    x8 bq[DSTEPS];
+    auto qk = [&](const uint16_t* sK, floatx16 (&s)[2]) {
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[kb][r] = 0.f;
+        const int krow_i = 32 * kb + l32;
+        const uint16_t* krow = sK + krow_i * DH;
+        const int ksw = SM::kswz(krow_i);
+#pragma unroll
+        for (int ds = 0; ds < DSTEPS; ++ds) {
+          const x8 ak = __builtin_bit_cast(x8, *reinterpret_cast<const uint4*>(krow + ((2 * ds + h) ^ ksw) * 8));
+          s[kb] = ST::mfma(ak, bq[ds], s[kb]);
+        }
+      }
+    };
+
+    // Scores in base-2 units (MOD) or still to be multiplied by scale * log2(e); -inf where a row is not seen.
+    // Register r of s[kb] is row 32 * kb + 8 * (r / 4) + 4 * h + r % 4 of the tile.
+    auto finish_scores = [&](int t, floatx16 (&s)[2]) {
+      const int key0 = t * kTileRows;
+      if constexpr (MOD) {
+        if (sc.cap_log2e > 0.f) {
+          // cap * tanh(x) = cap * (1 - 2 / (1 + e^(2x))): off by cap * 2^-23 at most, which a probability's rounding to 16 bits covers
+#pragma unroll
+          for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+              const float e = __builtin_amdgcn_exp2f(s[kb][r] * sc.cap_in);
+              s[kb][r] = __builtin_fmaf(-2.f * sc.cap_log2e, __builtin_amdgcn_rcpf(1.f + e), sc.cap_log2e);
+            }
+        } else {
+#pragma unroll
+          for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) s[kb][r] *= sc.scale_log2e;
+        }
+      }
+      if (!partly_seen(t)) {
+        if constexpr (MOD) {
+          if (sc.slopes != nullptr) {   // rows in front of every query: slope * (p_i - key)
+            const float bias0 = slope2 * static_cast<float>(p_i - key0 - 4 * h);
+#pragma unroll
+            for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+              for (int r = 0; r < 16; ++r)
+                s[kb][r] += __builtin_fmaf(slope2, static_cast<float>(32 * kb + 8 * (r / 4) + r % 4), -bias0);
+          }
+        }
+        return;
+      }
+      const unsigned long long bits = seen_rows(sc, b, token, P, key0, kend);
+      if (positions) {
+        const int key = key0 + lane;
+        int pos = key;
+        if (key >= P && key < kend) pos = P + offset_of(sc, b, key - P);
+        __builtin_amdgcn_wave_barrier();
+        s_pos[lane] = pos;
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+      }
+      const int window = sc.window > 0 ? sc.window : 0x7FFFFFFF;
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb) {
+        const uint32_t w = static_cast<uint32_t>(bits >> (32 * kb)) >> (4 * h);
+#pragma unroll
+        for (int q4 = 0; q4 < 4; ++q4) {
+          int4 pos = make_int4(0, 0, 0, 0);
+          if (positions) pos = *reinterpret_cast<const int4*>(s_pos + 32 * kb + 8 * q4 + 4 * h);
+          const int ps[4] = {pos.x, pos.y, pos.z, pos.w};
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const int r = 4 * q4 + e;
+            bool seen = (w >> (8 * q4 + e)) & 1u;
+            if (positions) {
+              const int apart = p_i - ps[e];
+              seen = seen && apart < window;
+              if constexpr (MOD) s[kb][r] = __builtin_fmaf(-slope2, fabsf(static_cast<float>(apart)), s[kb][r]);
+            }
+            s[kb][r] = seen ? s[kb][r] : kNoScore;
+          }
+        }
+      }
+    };
+    // Rows of tile t that this lane's query sees, as bits (again; for the rare tile with values that are not finite).
+    auto seen_bits = [&](int t) {
+      unsigned long long bits = seen_rows(sc, b, token, P, t * kTileRows, kend);
+      if (sc.window > 0) {
+        for (int k = 0; k < kTileRows; ++k) {
+          const int key = t * kTileRows + k;
+          const int pos = key < P || key >= kend ? key : P + offset_of(sc, b, key - P);
+          if (p_i - pos >= sc.window) bits &= ~(1ull << k);
+        }
+      }
+      return bits;
+    };
+
+    // V of a tile that not every row sees: are all values finite?  (Entered and left by all wavefronts together.)
+    auto clean_v = [&](int t, int st) {
+      uint4* const v = reinterpret_cast<uint4*>(stage_v(st));
+      uint32_t any = 0;
+#pragma unroll
+      for (int c = 0; c < SM::T_ELEMS / 8 / kWgThreads; ++c) {
+        const uint4 u = v[c * kWgThreads + tid];
+        any |= ST::not_finite(u.x) | ST::not_finite(u.y) | ST::not_finite(u.z) | ST::not_finite(u.w);
+      }
+      if (!__syncthreads_or(any != 0u)) return;
+      if (tid < 2) s_bad[tid] = 0u;
+      __syncthreads();
+      for (int c = 0; c < SM::T_ELEMS / 8 / kWgThreads; ++c) {
+        const int chunk = c * kWgThreads + tid;
+        uint4 u = v[chunk];
+        uint32_t* const w = reinterpret_cast<uint32_t*>(&u);
+        uint32_t found = 0;
+        for (int e = 0; e < 4; ++e) {
+          const uint32_t bad = ST::not_finite(w[e]);
+          found |= bad;
+          if (bad & 1u) w[e] &= 0xFFFF0000u;
+          if (bad & 2u) w[e] &= 0x0000FFFFu;
+        }
+        if (found) {
+          v[chunk] = u;
+          const int row = chunk / CPR;
+          atomicOr(&s_bad[row >> 5], 1u << (row & 31));
+        }
+      }
+      __syncthreads();
+      const unsigned long long bad = s_bad[0] | (static_cast<unsigned long long>(s_bad[1]) << 32);
+      if (seen_bits(t) & bad) l_run = __builtin_nanf("");
+    };
+
+    // One step, tile t = t_begin + i, whose finished scores are in s: loads of K(t + 2) and V(t + 1), scores of tile t + 1,
+    // softmax of tile t, O^T += V(t)^T . P^T.
+    auto step = [&](int i, floatx16 (&s)[2], floatx16 (&s_nxt)[2], auto has_next) {
+      constexpr bool kHasNext = decltype(has_next)::value;
+      const int t = t_begin + i;
+      if (partly_seen(t)) clean_v(t, i & 1);
+      if constexpr (kHasNext) {
+        if (loader) {
+          entries_landed();
+          uint32_t next_rows[LOADS];
+          if (i + 2 < nt) {
+            rows_of(t + 2, next_rows);
+            load_k(next_rows, i & 1);
+          }
+          load_v(v_rows, (i + 1) & 1);
+          if (i + 3 < nt) load_entries(t + 3);
+#pragma unroll
+          for (int j = 0; j < LOADS; ++j) v_rows[j] = next_rows[j];
+        }
+      }
+      if (works) {
+        const uint16_t* sV = stage_v(i & 1);
+        x8 pb[2][2];
+        float mx = kNoScore;
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) mx = fmaxf(mx, s[kb][r]);
+        {
+          const int mi = __float_as_int(mx);
+          const auto sw = __builtin_amdgcn_permlane32_swap(mi, mi, false, false);
+          mx = fmaxf(__int_as_float(static_cast<int>(sw[0])), __int_as_float(static_cast<int>(sw[1])));
+        }
+        const float c2 = MOD ? 1.f : sc.scale_log2e;
+        const float m_new = fmaxf(m_run, MOD ? mx : mx * c2);
+        const float m_safe = m_new == kNoScore ? 0.f : m_new;
+        const float alpha = __builtin_amdgcn_exp2f(m_run - m_safe);
+        m_run = m_new;
+        if (__ballot(alpha != 1.f) != 0ull) {
+#pragma unroll
+          for (int db = 0; db < DB; ++db)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) o[db][r] *= alpha;
+        }
+        if constexpr (kHasNext) qk(stage_k((i + 1) & 1), s_nxt);
+        {
+          // (probabilities are rounded to the storage type for the matrix product, the denominator sums them unrounded)
+          float sum0 = 0.f, sum1 = 0.f;
+#pragma unroll
+          for (int kb = 0; kb < 2; ++kb) {
+#pragma unroll
+            for (int sp = 0; sp < 2; ++sp) {
+              x8 pk;
+#pragma unroll
+              for (int e = 0; e < 8; ++e) {
+                const float v = s[kb][8 * sp + e];
+                const float p = __builtin_amdgcn_exp2f(MOD ? v - m_safe : __builtin_fmaf(v, c2, -m_safe));
+                if (e & 1) sum1 += p; else sum0 += p;
+                pk[e] = static_cast<typename ST::x1>(p);
+              }
+              pb[kb][sp] = pk;
+            }
+          }
+          l_run = l_run * alpha + (sum0 + sum1);
+        }
+        if constexpr (kHasNext) finish_scores(t + 1, s_nxt);
+
+        // ---- O^T += V^T . P^T
+        const int i16 = lane & 15;
+        const int dhblk = (lane >> 4) & 1;
+        const int vrow_l = 4 * h + (i16 >> 2);
+        const int vsw = SM::vswz(vrow_l);
+        const int vch = 2 * dhblk + ((i16 & 3) >> 1);
+        const int vsub = (i16 & 1) * 4;
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb) {
+#pragma unroll
+          for (int sp = 0; sp < 2; ++sp) {
+#pragma unroll
+            for (int db = 0; db < DB; ++db) {
+              const uint16_t* vp = sV + (32 * kb + 16 * sp + vrow_l) * DH + ((4 * db + vch) ^ vsw) * 8 + vsub;
+              const short4v lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) short4v*)(vp));
+              const short4v hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) short4v*)(vp + 8 * DH));
+              const short8v both = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+              o[db] = ST::mfma(__builtin_bit_cast(x8, both), pb[kb][sp], o[db]);
+            }
+          }
+        }
+        // (the two reads of a fragment run two matrix instructions ahead)
+        __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
+#pragma unroll
+        for (int g_ = 0; g_ < 4 * DB - 2; ++g_) {
+          __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+          __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+        }
+        __builtin_amdgcn_sched_group_barrier(0x008, 2, 0);
+      }
+      tile_landed();
+    };
+
+    // ---- prologue: page entries of the first two tiles, their rows, this lane's query
+    if (loader) {
+      load_entries(t_begin);
+      entries_landed();
+      uint32_t rows0[LOADS];
+      rows_of(t_begin, rows0);
+      load_k(rows0, 0);
+      load_v(rows0, 0);
+    }
+    {
+      const uint16_t* qp = a.q.p + static_cast<int64_t>(b) * a.q.sb + static_cast<int64_t>(token) * a.q.st + static_cast<int64_t>(head) * a.q.sh + 8 * h;
+      u32x4 qv[DSTEPS];
+#pragma unroll
+      for (int ds = 0; ds < DSTEPS; ++ds) {
+        qv[ds] = u32x4{0, 0, 0, 0};
+        if (valid) qv[ds] = *reinterpret_cast<const u32x4*>(qp + 16 * ds);
+      }
+      if (loader && nt > 1) load_entries(t_begin + 1);
+      // the compiler's waits for these loads stand here, not inside the loop
+#pragma unroll
+      for (int ds = 0; ds < DSTEPS; ds += 4) asm volatile("" : "+v"(qv[ds]), "+v"(qv[ds + 1]), "+v"(qv[ds + 2]), "+v"(qv[ds + 3]));
+#pragma unroll
+      for (int ds = 0; ds < DSTEPS; ++ds) bq[ds] = __builtin_bit_cast(x8, qv[ds]);
+    }
+    if (loader && nt > 1) {
+      entries_landed();
+      rows_of(t_begin + 1, v_rows);
+      load_k(v_rows, 1);
+      if (nt > 2) load_entries(t_begin + 2);
+    }
+    floatx16 s_a[2], s_b[2];
+    tile_landed();
+    if (works) {
+      qk(stage_k(0), s_a);
+      finish_scores(t_begin, s_a);
+    }
+    __syncthreads();   // K stage 0 is free
+    {
+      constexpr std::true_type more{};
+      constexpr std::false_type last{};
+      int i = 0;
+      for (; i + 2 < nt; i += 2) {
+        step(i, s_a, s_b, more);
+        step(i + 1, s_b, s_a, more);
+      }
+      if (i + 1 < nt) {
+        step(i, s_a, s_b, more);
+        step(i + 1, s_b, s_a, last);
+      } else {
+        step(i, s_a, s_b, last);
+      }
+    }
+
+    // ---- what became of the rows
+    float l_tot;
+    {
+      const int li = __float_as_int(l_run);
+      const auto sw = __builtin_amdgcn_permlane32_swap(li, li, false, false);
+      l_tot = __int_as_float(static_cast<int>(sw[0])) + __int_as_float(static_cast<int>(sw[1]));
+    }
+    // (worked out again from a lane index that the compiler cannot trace back: it would keep the addresses across the loop)
+    int l32_e = l32;
+    asm volatile("" : "+v"(l32_e));
+    const int rho_e = wrow0 + l32_e;
+    if (rho_e < rows) {
+      if (whole) {
+        const int token_e = div_g(rho_e, a.inv_g);
+        const int head_e = g * G + rho_e - token_e * G;
+        const float inv = l_tot == 0.f ? 0.f : 1.f / l_tot;   // a row that sees nothing
+        uint16_t* op = a.out.p + static_cast<int64_t>(b) * a.out.sb + static_cast<int64_t>(token_e) * a.out.st + static_cast<int64_t>(head_e) * a.out.sh;
+#pragma unroll
+        for (int db = 0; db < DB; ++db)
+#pragma unroll
+          for (int q4 = 0; q4 < 4; ++q4) {
+            x4 v;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] = static_cast<typename ST::x1>(o[db][4 * q4 + e] * inv);
+            *reinterpret_cast<x4*>(op + 32 * db + 8 * q4 + 4 * h) = v;
+          }
+        if (a.lse != nullptr && h == 0)
+          a.lse[(static_cast<size_t>(b) * sc.N + token_e) * (a.Hkv * G) + head_e] = (m_run + __builtin_amdgcn_logf(l_tot)) * kLn2F;
+      } else {
+        const int slot = 2 * share + (first_piece ? 0 : 1);
+        const int r = rho_e - row0;
+        float* po = a.part_o + (static_cast<size_t>(slot) * (DH / 8) * a.rows_slot + r) * 8 + 4 * h;
+#pragma unroll
+        for (int db = 0; db < DB; ++db)
+#pragma unroll
+          for (int q4 = 0; q4 < 4; ++q4) {
+            float4 v = make_float4(o[db][4 * q4], o[db][4 * q4 + 1], o[db][4 * q4 + 2], o[db][4 * q4 + 3]);
+            *reinterpret_cast<float4*>(po + static_cast<size_t>(4 * db + q4) * a.rows_slot * 8) = v;
+          }
+        if (h == 0) {
+          a.part_m[static_cast<size_t>(slot) * a.rows_slot + r] = m_run;
+          a.part_l[static_cast<size_t>(slot) * a.rows_slot + r] = l_tot;
+        }
+      }
+    }
+    // the row tile goes on behind this share, and begins in it: the merge at this share's end joins it
+    if (at + take < tiles && at == 0 && tid == 0) {
+      const int last_share = (x + tiles - 1) / share_tiles;
+      const int count = rows - row0 < kRowTile ? rows - row0 : kRowTile;
+      a.cut[share] = make_int4(b * a.Hkv + g, row0, count, last_share | (first_piece ? 0 : 1 << 30));
+    }
+
+    // ---- on to the next row tile
+    x += split ? take : 1;
+    at = 0;
+    first_piece = false;
+    if (x < x_end) {
+      ++rt;
+      if (rt * kRowTile >= rows) {
+        rt = 0;
+        if (++g == a.Hkv) {
+          g = 0;
+          do {   // (x < x_end: there is another sequence with new tokens)
+            ++b;
+            clamped_lengths(a.c, sc.prefix_len[b], sc.n_new[b], sc.max_prefix_len, sc.N, &P, &n);
+          } while (n == 0);
+        }
+      }
+      __syncthreads();   // (s_bad and the stages are free)
+    }
+  }
+}
+
+// Joins the pieces of a row tile that begins in share blockIdx.y and ends in another one.
+//   out = sum_s 2^(m_s - M) O_s / sum_s 2^(m_s - M) l_s
+// One thread per (row, 4 values); pieces are read in the order in which they lie (thread = (slab, row, half)) and the rows
+// turned through LDS.
+template <bool F16, int DH>
+__global__ __launch_bounds__(256) void paged_attention_join_kernel(PagedAttnArgs a) {
+  using ST = Storage<F16>;
+  using x4 = typename ST::x4;
+  constexpr int QPR = DH / 4;
+  constexpr int RPW = 256 / QPR;
+  __shared__ x4 s_out[RPW][QPR];
+  const int share = blockIdx.y;
+  const int4 cut = a.cut[share];
+  if (static_cast<int>(blockIdx.x) * RPW >= cut.z) return;
+  const int last = cut.w & 0x3FFFFFFF;
+  const int t = threadIdx.x;
+  const int h = t & 1;
+  const int r = (t >> 1) % RPW;
+  const int slab = t / (2 * RPW);
+  const int c = 2 * slab + h;
+  int row = blockIdx.x * RPW + r;
+  const bool valid = row < cut.z;
+  row = valid ? row : cut.z - 1;
+  float M = kNoScore, den = 0.f;
+  float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+  const int pieces = last - share + 1;
+  for (int s0 = 0; s0 < pieces; s0 += 8) {
+    float ms[8], ls[8];
+    float4 vs[8];
+#pragma unroll
+    for (int u = 0; u < 8; ++u) {
+      ms[u] = kNoScore;
+      ls[u] = 0.f;
+      vs[u] = make_float4(0.f, 0.f, 0.f, 0.f);
+      if (s0 + u < pieces) {
+        const int slot = 2 * (share + s0 + u) + (s0 + u == 0 ? cut.w >> 30 : 0);
+        const size_t at = static_cast<size_t>(slot) * a.rows_slot;
+        ms[u] = a.part_m[at + row];
+        ls[u] = a.part_l[at + row];
+        vs[u] = *reinterpret_cast<const float4*>(a.part_o + (at * (DH / 8) + static_cast<size_t>(slab) * a.rows_slot + row) * 8 + 4 * h);
+      }
+    }
+    float Mb = M;
+#pragma unroll
+    for (int u = 0; u < 8; ++u) Mb = fmaxf(Mb, ms[u]);
+    const float safe = Mb == kNoScore ? 0.f : Mb;   // (a piece that saw nothing has no weight; one with a NaN keeps it)
+    const float keep = __builtin_amdgcn_exp2f(M - safe);
+    M = Mb;
+    den *= keep;
+    acc.x *= keep; acc.y *= keep; acc.z *= keep; acc.w *= keep;
+#pragma unroll
+    for (int u = 0; u < 8; ++u) {
+      const float w = __builtin_amdgcn_exp2f(ms[u] - safe);
+      den = __builtin_fmaf(w, ls[u], den);
+      acc.x = __builtin_fmaf(w, vs[u].x, acc.x); acc.y = __builtin_fmaf(w, vs[u].y, acc.y);
+      acc.z = __builtin_fmaf(w, vs[u].z, acc.z); acc.w = __builtin_fmaf(w, vs[u].w, acc.w);
+    }
+  }
+  const float inv = den == 0.f ? 0.f : 1.f / den;
+  x4 v;
+  v[0] = static_cast<typename ST::x1>(acc.x * inv);
+  v[1] = static_cast<typename ST::x1>(acc.y * inv);
+  v[2] = static_cast<typename ST::x1>(acc.z * inv);
+  v[3] = static_cast<typename ST::x1>(acc.w * inv);
+  s_out[r][c] = v;
+  const int b = cut.x / a.Hkv;
+  const int g = cut.x - b * a.Hkv;
+  if (a.lse != nullptr && c == 0 && valid) {
+    const int rho = cut.y + row;
+    const int token = div_g(rho, a.inv_g);
+    a.lse[(static_cast<size_t>(b) * a.sc.N + token) * (a.Hkv * a.G) + g * a.G + rho - token * a.G] = (M + __builtin_amdgcn_logf(den)) * kLn2F;
+  }
+  __syncthreads();
+  const int r2 = t / QPR;
+  const int c2 = t - r2 * QPR;
+  const int row2 = blockIdx.x * RPW + r2;
+  if (row2 < cut.z) {
+    const int rho = cut.y + row2;
+    const int token = div_g(rho, a.inv_g);
+    uint16_t* op = a.out.p + static_cast<int64_t>(b) * a.out.sb + static_cast<int64_t>(token) * a.out.st +
+                   static_cast<int64_t>(g * a.G + rho - token * a.G) * a.out.sh;
+    *reinterpret_cast<x4*>(op + 4 * c2) = s_out[r2][c2];
+  }
+}
+
+template <bool F16, int DH, int NW, bool MOD>
+hipError_t launch_paged_one(const PagedAttnArgs& a, hipStream_t s) {
+  auto kern = paged_attention_kernel<F16, DH, NW, MOD>;
+  static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize,
+                                                     PagedSmem<DH>::BYTES);
+  if (attr != hipSuccess) return attr;
+  hipLaunchKernelGGL(kern, dim3((a.slots + 7) / 8 * 8), dim3(64 * NW), PagedSmem<DH>::BYTES, s, a);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess || a.cut == nullptr) return e;
+  constexpr int RPW = 256 / (DH / 4);
+  hipLaunchKernelGGL((paged_attention_join_kernel<F16, DH>), dim3((a.rows_slot + RPW - 1) / RPW, a.slots), dim3(256), 0, s, a);
+  return hipGetLastError();
+}
+
+template <bool F16, int DH>
+hipError_t launch_paged_dh(const PagedAttnArgs& a, int waves, hipStream_t s) {
+  const bool mod = a.sc.cap_log2e > 0.f || a.sc.slopes != nullptr;
+  if constexpr (DH != 256) {
+    if (waves == 8) return mod ? launch_paged_one<F16, DH, 8, true>(a, s) : launch_paged_one<F16, DH, 8, false>(a, s);
+  }
+  return mod ? launch_paged_one<F16, DH, 4, true>(a, s) : launch_paged_one<F16, DH, 4, false>(a, s);
+}
+
+template <bool F16>
+hipError_t launch_paged(const PagedAttnArgs& a, int Dh, int waves, hipStream_t s) {
+  switch (Dh) {
+    case 64: return launch_paged_dh<F16, 64>(a, waves, s);
+    case 128: return launch_paged_dh<F16, 128>(a, waves, s);
+    default: return launch_paged_dh<F16, 256>(a, waves, s);
+  }
+}
+
+}  // namespace
+
+}  // namespace talon

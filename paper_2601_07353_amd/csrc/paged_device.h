@@ -1,0 +1,74 @@
+// Device helpers of the calls on a paged cache.
+#pragma once
+
+#include "device_utils.h"
+#include "paged_internal.h"
+
+namespace talon {
+
+constexpr float kNoScore = -__builtin_huge_valf();
+constexpr float kLog2eF = 1.4426950408889634f;
+constexpr float kLn2F = 0.6931471805599453f;
+
+// x / G for 0 <= x < 2^24, G <= 128: exact, since x * (inv_g * G - 2^32) < 2^32.
+__device__ __forceinline__ int div_g(int x, uint32_t inv_g) { return inv_g == 0u ? x : static_cast<int>(__umulhi(static_cast<uint32_t>(x), inv_g)); }
+
+// Rows that a sequence has in the cache and rows that are new, whatever the device's numbers say: neither
+// points beyond what the call or the page table allows for.
+__device__ __forceinline__ void clamped_lengths(const PagedRows& c, int prefix, int fresh, int max_prefix, int N, int* P, int* n) {
+  int p = prefix < 0 ? 0 : (prefix > max_prefix ? max_prefix : prefix);
+  p = p < c.capacity ? p : c.capacity;
+  int m = fresh < 0 ? 0 : (fresh > N ? N : fresh);
+  *P = p;
+  *n = m < c.capacity - p ? m : c.capacity - p;
+}
+
+__device__ __forceinline__ void report(const PagedRows& c, int b, uint32_t bit) { atomicOr(&c.status[b], bit); }
+
+// First chunk of (row's page entry, row, KV head); an entry that names no page of the pool is page 0 (the caller reports it).
+__device__ __forceinline__ uint32_t row_chunk(const PagedRows& c, uint32_t entry, int row, int g) {
+  const uint32_t page = entry < c.num_pages ? entry : 0u;
+  const uint32_t slot = static_cast<uint32_t>(row) & ((1u << c.page_shift) - 1u);
+  return page * c.page_chunks + slot * c.token_chunks + static_cast<uint32_t>(g) * c.head_chunks;
+}
+
+__device__ __forceinline__ uint32_t page_entry(const PagedRows& c, int b, int row) {
+  return static_cast<uint32_t>(c.table[static_cast<size_t>(b) * c.max_pages + (row >> c.page_shift)]);
+}
+
+template <class T>
+__device__ __forceinline__ T* chunk_at(T* base, uint32_t chunk) { return base + static_cast<size_t>(chunk) * 8; }
+
+// Which of the 64 rows from `row0` on the new token `i` of a sequence may see, by its mask words or causally (not yet by a
+// window), as bits; rows from `end` on are never seen.
+__device__ __forceinline__ unsigned long long seen_rows(const ScoreArgs& s, int b, int i, int P, int row0, int end) {
+  unsigned long long bits;
+  const int d = row0 - P;   // new token that row0 is
+  if (s.mask == nullptr) {
+    const int count = P + i + 1 - row0;
+    bits = count >= 64 ? ~0ull : (count <= 0 ? 0ull : (1ull << count) - 1ull);
+  } else {
+    const uint64_t* w = s.mask + (static_cast<size_t>(b) * s.N + i) * s.words;
+    if (d >= 0) {
+      const int at = d >> 6, shift = d & 63;
+      bits = at < s.words ? w[at] >> shift : 0ull;
+      if (shift != 0 && at + 1 < s.words) bits |= w[at + 1] << (64 - shift);
+    } else if (d > -64) {
+      bits = (w[0] << -d) | ((1ull << -d) - 1ull);
+    } else {
+      bits = ~0ull;
+    }
+  }
+  const int left = end - row0;
+  if (left < 64) bits &= left <= 0 ? 0ull : (1ull << left) - 1ull;
+  return bits;
+}
+
+// Position of new token i relative to the prefix.
+__device__ __forceinline__ int offset_of(const ScoreArgs& s, int b, int i) {
+  if (s.offset == nullptr) return i;
+  const int o = s.offset[static_cast<size_t>(b) * s.N + i];
+  return o < 0 ? 0 : o;
+}
+
+}  // namespace talon

@@ -1,0 +1,52 @@
+// Launch plan of attention over a paged cache.  Host code without HIP, so that tests can evaluate it on a machine without a GPU.
+#pragma once
+
+#include <stddef.h>
+#include <stdint.h>
+
+namespace talon {
+
+struct PagedPlan {
+  int waves;        // wavefronts per workgroup
+  int split;        // 1: row tiles are cut into shares; 0: a workgroup per row tile, nothing to join
+  int slots;        // workgroups
+  int least;        // fewest key tiles of a share
+  int rows_slot;    // rows of a partial result
+  long long tiles;  // key tiles of the call if every sequence is as long as it may be
+  size_t off_m, off_l, off_cut, bytes;   // workspace: outputs, maxima, denominators, cuts
+};
+
+constexpr int kPagedTile = 64;
+constexpr int kPagedWholeTiles = 4;   // up to so many key tiles a row tile is not cut
+constexpr int kPagedLeast = 2;        // fewest key tiles of a share
+
+inline PagedPlan paged_plan(int B, int N, int Hq, int Hkv, int Dh, int max_prefix_len) {
+  PagedPlan p = {};
+  const long long rows = static_cast<long long>(N) * (Hq / Hkv);
+  p.waves = Dh != 256 && rows >= 512 ? 8 : 4;
+  const int row_tile = 32 * p.waves;
+  const long long items = static_cast<long long>(B) * Hkv * ((rows + row_tile - 1) / row_tile);
+  const long long most = (static_cast<long long>(max_prefix_len) + N + kPagedTile - 1) / kPagedTile;
+  p.tiles = items * most;
+  p.rows_slot = static_cast<int>(rows < row_tile ? rows : row_tile);
+  p.split = most > kPagedWholeTiles ? 1 : 0;
+  if (!p.split) {
+    p.slots = static_cast<int>(items < (1ll << 30) ? items : (1ll << 30));
+    p.least = 1;
+    p.bytes = 256;   // nothing is staged, keep a token size
+    return p;
+  }
+  p.least = kPagedLeast;
+  const long long slots = p.waves == 8 || Dh == 256 ? 256 : 512;   // workgroups that the device holds at once
+  const long long enough = (p.tiles + p.least - 1) / p.least;
+  p.slots = static_cast<int>(enough < slots ? enough : slots);
+  const size_t slot_rows = 2 * static_cast<size_t>(p.slots) * p.rows_slot;
+  auto up = [](size_t x) { return (x + 255) / 256 * 256; };
+  p.off_m = up(slot_rows * Dh * sizeof(float));
+  p.off_l = p.off_m + up(slot_rows * sizeof(float));
+  p.off_cut = p.off_l + up(slot_rows * sizeof(float));
+  p.bytes = p.off_cut + up(static_cast<size_t>(p.slots) * 16);
+  return p;
+}
+
+}  // namespace talon

@@ -1,0 +1,452 @@
+// Rows of a paged cache: written with rotated keys, moved behind the prefix, dropped and moved together.  All of it is
+// bound by the bytes that it moves.
+#include "paged_device.h"
+
+namespace talon {
+
+namespace {
+
+__device__ __forceinline__ float to_float(uint16_t v, bool f16) {
+  if (f16) return static_cast<float>(__builtin_bit_cast(_Float16, v));
+  return __uint_as_float(static_cast<uint32_t>(v) << 16);
+}
+__device__ __forceinline__ uint16_t from_float(float v, bool f16) {
+  if (f16) return __builtin_bit_cast(uint16_t, static_cast<_Float16>(v));
+  return __builtin_bit_cast(uint16_t, static_cast<__bf16>(v));
+}
+
+union Chunk {
+  uint4 v;
+  uint16_t e[8];
+};
+
+// ---- rotary positions and the write into the pages.
+// angle(token, f) = (base + pos[axis(f)][token]) * inv_freq[f];  (x1, x2) -> (x1 cos - x2 sin, x2 cos + x1 sin)
+// A workgroup takes TOKENS tokens.  First the angles' sines and cosines, one (token, f) per thread, to LDS: the product and its
+// reduction to one turn are formed in 64 bits (a position of 10^5 in fp32 has lost 2^-8 of a turn), the rest in fp32.  Then the
+// heads' values, two chunks of 16 bytes per thread: the eight first and the eight second values of eight pairs, so that a
+// value is read and written by one thread and q may be rotated in place.
+template <bool F16, int TOKENS>
+__global__ __launch_bounds__(256) void rotary_store_kernel(RotaryArgs a) {
+  extern __shared__ float2 s_turn[];   // [TOKENS][pairs] cosine, sine
+  const int b = blockIdx.y;
+  const int i0 = blockIdx.x * TOKENS;
+  const int tid = threadIdx.x;
+  int P, n;
+  clamped_lengths(a.c, a.prefix_len[b], a.n_new[b], a.c.capacity, a.N, &P, &n);
+  if (blockIdx.x == 0 && tid == 0) {
+    const int want = a.n_new[b] < a.N ? a.n_new[b] : a.N;
+    if (want > n) report(a.c, b, TALON_STATUS_BAD_PAGE);   // rows beyond the page table are not written
+  }
+  if (i0 >= n) return;
+  const int base = a.base != nullptr ? a.base[b] : 0;
+  for (int x = tid; x < TOKENS * a.pairs; x += 256) {
+    const int t = x / a.pairs, f = x - t * a.pairs;
+    if (i0 + t < n) {
+      int axis = a.axis != nullptr ? a.axis[f] : 0;
+      axis = axis < 0 ? 0 : (axis < a.axes ? axis : a.axes - 1);
+      const double at = static_cast<double>(base) + static_cast<double>(a.pos[(static_cast<size_t>(axis) * a.B + b) * a.N + i0 + t]);
+      const double turns = at * (static_cast<double>(a.inv_freq[f]) * 0.15915494309189535);
+      float sine, cosine;
+      sincospif(static_cast<float>(2.0 * (turns - rint(turns))), &sine, &cosine);
+      s_turn[x] = make_float2(cosine, sine);
+    }
+  }
+  __syncthreads();
+  // units of a head: groups of eight pairs, then groups of eight values that are copied
+  const int groups = (a.pairs + 7) / 8;
+  const int rest = a.Dh - 2 * a.pairs;
+  const int units = groups + (rest + 7) / 8;
+  const int copies = (a.Dh + 7) / 8;             // of a value head
+  const int per_token = (a.Hq + a.Hkv) * units + a.Hkv * copies;
+  const bool whole = a.pairs % 8 == 0;           // (else value by value)
+  for (int x = tid; x < TOKENS * per_token; x += 256) {
+    const int t = x / per_token;
+    int u = x - t * per_token;
+    const int i = i0 + t;
+    if (i >= n) break;
+    const int rotated = (a.Hq + a.Hkv) * units;
+    int head, unit;
+    bool is_q = false, is_v = false;
+    if (u < rotated) {
+      head = u / units;
+      unit = u - head * units;
+      is_q = head < a.Hq;
+      if (!is_q) head -= a.Hq;
+    } else {
+      u -= rotated;
+      head = u / copies;
+      unit = u - head * copies;
+      is_v = true;
+    }
+    const RowsView& from = is_q ? a.q : (is_v ? a.v : a.k);
+    const uint16_t* src = from.p + static_cast<int64_t>(b) * from.sb + static_cast<int64_t>(i) * from.st + static_cast<int64_t>(head) * from.sh;
+    uint16_t* dst;
+    if (is_q) {
+      dst = a.q_out.p + static_cast<int64_t>(b) * a.q_out.sb + static_cast<int64_t>(i) * a.q_out.st + static_cast<int64_t>(head) * a.q_out.sh;
+    } else {
+      const uint32_t entry = page_entry(a.c, b, P + i);
+      if (entry >= a.c.num_pages) {   // nowhere to write to
+        report(a.c, b, TALON_STATUS_BAD_PAGE);
+        continue;
+      }
+      dst = chunk_at(static_cast<uint16_t*>(is_v ? a.c.v : a.c.k), row_chunk(a.c, entry, P + i, head));
+    }
+    if (is_v) {
+      *reinterpret_cast<uint4*>(dst + 8 * unit) = *reinterpret_cast<const uint4*>(src + 8 * unit);
+    } else if (unit < groups) {
+      const float2* turn = s_turn + t * a.pairs + 8 * unit;
+      if (whole) {
+        const int one = a.interleaved ? 16 * unit : 8 * unit;
+        const int two = a.interleaved ? 16 * unit + 8 : a.pairs + 8 * unit;
+        Chunk c1, c2, r1, r2;
+        c1.v = *reinterpret_cast<const uint4*>(src + one);
+        c2.v = *reinterpret_cast<const uint4*>(src + two);
+        if (a.interleaved) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const float2 t1 = turn[e], t2 = turn[4 + e];
+            const float x1 = to_float(c1.e[2 * e], F16), y1 = to_float(c1.e[2 * e + 1], F16);
+            const float x2 = to_float(c2.e[2 * e], F16), y2 = to_float(c2.e[2 * e + 1], F16);
+            r1.e[2 * e] = from_float(x1 * t1.x - y1 * t1.y, F16);
+            r1.e[2 * e + 1] = from_float(y1 * t1.x + x1 * t1.y, F16);
+            r2.e[2 * e] = from_float(x2 * t2.x - y2 * t2.y, F16);
+            r2.e[2 * e + 1] = from_float(y2 * t2.x + x2 * t2.y, F16);
+          }
+        } else {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            const float2 t1 = turn[e];
+            const float x1 = to_float(c1.e[e], F16), y1 = to_float(c2.e[e], F16);
+            r1.e[e] = from_float(x1 * t1.x - y1 * t1.y, F16);
+            r2.e[e] = from_float(y1 * t1.x + x1 * t1.y, F16);
+          }
+        }
+        *reinterpret_cast<uint4*>(dst + one) = r1.v;
+        *reinterpret_cast<uint4*>(dst + two) = r2.v;
+      } else {
+        for (int e = 0; e < 8 && 8 * unit + e < a.pairs; ++e) {
+          const int f = 8 * unit + e;
+          const int one = a.interleaved ? 2 * f : f, two = a.interleaved ? 2 * f + 1 : f + a.pairs;
+          const float x1 = to_float(src[one], F16), y1 = to_float(src[two], F16);
+          dst[one] = from_float(x1 * turn[e].x - y1 * turn[e].y, F16);
+          dst[two] = from_float(y1 * turn[e].x + x1 * turn[e].y, F16);
+        }
+      }
+    } else {
+      const int d = 2 * a.pairs + 8 * (unit - groups);
+      if (whole) {
+        *reinterpret_cast<uint4*>(dst + d) = *reinterpret_cast<const uint4*>(src + d);
+      } else {
+        for (int e = 0; e < 8 && d + e < a.Dh; ++e) dst[d + e] = src[d + e];
+      }
+    }
+  }
+}
+
+// ---- the accepted path's rows to their places behind the prefix.
+// A workgroup has one (sequence, KV head) and 64 values of the rows of K or of V.  It reads all rows that move before it writes
+// any, so the order of the path does not matter; the first row (the root's) is at its place.
+constexpr int kPathMost = TALON_N_MAX;
+__global__ __launch_bounds__(256) void paged_compact_kernel(CompactArgs a) {
+  constexpr int kPer = kPathMost * 8 / 256;   // chunks of 8 values per thread
+  const int b = blockIdx.z, g = blockIdx.y;
+  const int groups = (a.Dh + 63) / 64;
+  const bool is_v = static_cast<int>(blockIdx.x) >= groups;
+  const int group = static_cast<int>(blockIdx.x) - (is_v ? groups : 0);
+  const int tid = threadIdx.x;
+  int len = a.accept_len[b];
+  len = len < 0 ? -1 : (len < a.N ? len : a.N - 1);
+  int P = a.prefix_len[b];
+  P = P < 0 ? 0 : (P < a.c.capacity ? P : a.c.capacity);
+  const int room = a.c.capacity - P;
+  if (blockIdx.x == 0 && g == 0 && tid == 0) {
+    a.new_prefix_len[b] = P + (len + 1 < room ? len + 1 : room);
+    if (len + 1 > room) report(a.c, b, TALON_STATUS_BAD_PAGE);
+  }
+  const int count = len + 1 < room ? len + 1 : room;   // rows 0 .. count - 1 of the path
+  uint16_t* const pool = static_cast<uint16_t*>(is_v ? a.c.v : a.c.k);
+  uint4 v[kPer];
+  uint32_t to[kPer];
+  uint32_t moved = 0;
+  const int col = group * 8 + (tid & 7);       // 16-byte chunk of the head
+#pragma unroll
+  for (int u = 0; u < kPer; ++u) {
+    const int j = (tid >> 3) + 32 * u;
+    to[u] = 0;
+    v[u] = make_uint4(0, 0, 0, 0);
+    if (j < count && col * 8 < a.Dh) {
+      const int node = a.path[static_cast<size_t>(b) * a.N + j];
+      if (node >= 0 && node < a.N && node != j) {
+        bool bad = P + node >= a.c.capacity;
+        if (!bad) {
+          const uint32_t from = page_entry(a.c, b, P + node), dest = page_entry(a.c, b, P + j);
+          bad = from >= a.c.num_pages || dest >= a.c.num_pages;
+          if (!bad) {
+            v[u] = *reinterpret_cast<const uint4*>(chunk_at(pool, row_chunk(a.c, from, P + node, g) + col));
+            to[u] = row_chunk(a.c, dest, P + j, g) + col;
+            moved |= 1u << u;
+          }
+        }
+        if (bad) report(a.c, b, TALON_STATUS_BAD_PAGE);
+      }
+    }
+  }
+  float w = 0.f;
+  float* const row = a.weights != nullptr ? a.weights + static_cast<size_t>(b) * a.stride_b + static_cast<size_t>(g) * a.stride_h : nullptr;
+  bool w_moves = false;
+  if (row != nullptr && blockIdx.x == 0 && tid < count) {
+    const int node = a.path[static_cast<size_t>(b) * a.N + tid];
+    w_moves = node >= 0 && node < a.N && node != tid && P + node < a.weight_rows && P + tid < a.weight_rows;
+    if (w_moves) w = row[P + node];
+  }
+  __syncthreads();
+#pragma unroll
+  for (int u = 0; u < kPer; ++u)
+    if (moved >> u & 1u) *reinterpret_cast<uint4*>(chunk_at(pool, to[u])) = v[u];
+  if (w_moves) row[P + tid] = w;
+}
+
+// ---- which rows stay: per (sequence, KV head) the first n_sink, the last n_recent and, of those between, the ones of largest
+// weight up to the budget; ties go to the lowest row.
+// One workgroup of 1024 threads.  The weight of the last one to stay is found digit by digit (11, 11 and 10 bits of the
+// order-preserving integer image, counts in LDS), then the rows are taken in order by prefix counts.  Up to 16384 rows lie in
+// registers, 16 a thread; longer ones are read again from the caches for every digit.
+constexpr int kSelectThreads = 1024;
+constexpr int kRowsPerThread = 16;
+constexpr int kSelectRows = kSelectThreads * kRowsPerThread;
+
+// (a weight that is no number is the least of all)
+__device__ __forceinline__ uint32_t weight_key(float w) { return w != w ? 0u : sortable_u32(w); }
+
+// Exclusive prefix sum over the 1024 threads of two counts packed in halves of 32 bits each (their totals stay below 2^31).
+__device__ __forceinline__ uint2 block_scan_two(uint2 v, uint2* s_wave, uint2* total) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const uint2 incl = make_uint2(static_cast<uint32_t>(wave_inclusive_scan_i32(static_cast<int>(v.x))),
+                                static_cast<uint32_t>(wave_inclusive_scan_i32(static_cast<int>(v.y))));
+  __syncthreads();
+  if (lane == 63) s_wave[wave] = incl;
+  __syncthreads();
+  uint2 before = make_uint2(0, 0), sum = make_uint2(0, 0);
+  for (int w = 0; w < kSelectThreads / 64; ++w) {
+    const uint2 t = s_wave[w];
+    if (w < wave) { before.x += t.x; before.y += t.y; }
+    sum.x += t.x; sum.y += t.y;
+  }
+  *total = sum;
+  return make_uint2(before.x + incl.x - v.x, before.y + incl.y - v.y);
+}
+
+__global__ __launch_bounds__(kSelectThreads) void evict_select_kernel(EvictArgs a) {
+  __shared__ uint32_t s_count[2048];
+  __shared__ uint2 s_wave[kSelectThreads / 64];
+  __shared__ uint32_t s_found[2];
+  const int b = blockIdx.y, g = blockIdx.x;
+  const int tid = threadIdx.x, lane = tid & 63;
+  int len = a.len[b];
+  len = len < 0 ? 0 : (len < a.max_len ? len : a.max_len);
+  len = len < a.src.capacity ? len : a.src.capacity;
+  const float* const w = a.weights + static_cast<size_t>(b) * a.stride_b + static_cast<size_t>(g) * a.stride_h;
+  float* const w_out = a.new_weights != nullptr ? a.new_weights + static_cast<size_t>(b) * a.new_stride_b + static_cast<size_t>(g) * a.new_stride_h : nullptr;
+  int32_t* const kept = a.kept + (static_cast<size_t>(b) * a.Hkv + g) * a.budget;
+  const int stays = len < a.budget ? len : a.budget;
+  if (g == 0 && tid == 0) a.new_len[b] = stays;
+  for (int m = stays + tid; m < a.budget; m += kSelectThreads) kept[m] = -1;
+  if (stays == len) {   // nothing is dropped
+    for (int m = tid; m < len; m += kSelectThreads) {
+      kept[m] = m;
+      if (w_out != nullptr && w_out != w) w_out[m] = w[m];
+    }
+    return;
+  }
+  const int lo = a.n_sink, hi = len - a.n_recent;                 // rows that the weights decide on
+  uint32_t need = static_cast<uint32_t>(a.budget - a.n_sink - a.n_recent);
+  const int blocks = (len + kSelectRows - 1) / kSelectRows;
+  uint32_t key[kRowsPerThread];
+  auto load = [&](int block) {
+    const int first = block * kSelectRows + tid * kRowsPerThread;
+#pragma unroll
+    for (int e = 0; e < kRowsPerThread; ++e) key[e] = first + e < len ? weight_key(w[first + e]) : 0u;
+  };
+  if (blocks == 1) load(0);
+  uint32_t prefix = 0, prefix_mask = 0;   // digits of the last one to stay that are known
+  if (need > 0) {
+    for (int digit = 0; digit < 3; ++digit) {
+      const int shift = digit == 0 ? 21 : (digit == 1 ? 10 : 0);
+      const uint32_t bins = digit == 2 ? 1024u : 2048u;
+      for (int i = tid; i < 2048; i += kSelectThreads) s_count[i] = 0u;
+      __syncthreads();
+      for (int block = 0; block < blocks; ++block) {
+        if (blocks > 1) load(block);
+        const int first = block * kSelectRows + tid * kRowsPerThread;
+#pragma unroll
+        for (int e = 0; e < kRowsPerThread; ++e) {
+          const int row = first + e;
+          const bool in = row >= lo && row < hi && (key[e] & prefix_mask) == prefix;
+          const uint32_t bin = key[e] >> shift & (bins - 1u);
+          // (a wavefront whose rows all fall into one bin, as zeros do, counts them at once)
+          const unsigned long long all = __ballot(in);
+          if (all == 0ull) continue;
+          const uint32_t common = static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(bin), __ffsll(static_cast<long long>(all)) - 1));
+          if (__ballot(in && bin != common) == 0ull) {
+            if (lane == 0) atomicAdd(&s_count[common], static_cast<uint32_t>(__popcll(all)));
+          } else if (in) {
+            atomicAdd(&s_count[bin], 1u);
+          }
+        }
+      }
+      __syncthreads();
+      // the bin, from the largest down, in which the need-th lies: two bins a thread, thread 0 has the largest
+      const uint32_t hi_bin = bins - 1u - 2u * tid, lo_bin = bins - 2u - 2u * tid;
+      const bool has = 2u * tid + 1u < bins;
+      const uint32_t c_hi = has ? s_count[hi_bin] : 0u, c_lo = has ? s_count[lo_bin] : 0u;
+      uint2 total;
+      const uint2 before = block_scan_two(make_uint2(c_hi + c_lo, 0u), s_wave, &total);
+      if (has) {
+        if (before.x < need && need <= before.x + c_hi) { s_found[0] = hi_bin; s_found[1] = need - before.x; }
+        else if (before.x + c_hi < need && need <= before.x + c_hi + c_lo) { s_found[0] = lo_bin; s_found[1] = need - before.x - c_hi; }
+      }
+      __syncthreads();
+      prefix |= s_found[0] << shift;
+      prefix_mask |= (bins - 1u) << shift;
+      need = s_found[1];
+    }
+  }
+  // rows above `prefix` stay, and of those equal to it the first `need`
+  const bool none = a.budget - a.n_sink - a.n_recent == 0;
+  uint32_t taken = 0, equal = 0;
+  for (int block = 0; block < blocks; ++block) {
+    if (blocks > 1) load(block);
+    const int first = block * kSelectRows + tid * kRowsPerThread;
+    uint32_t ties = 0;
+#pragma unroll
+    for (int e = 0; e < kRowsPerThread; ++e) {
+      const int row = first + e;
+      ties += !none && row >= lo && row < hi && key[e] == prefix ? 1u : 0u;
+    }
+    uint2 total;
+    uint2 before = block_scan_two(make_uint2(ties, 0u), s_wave, &total);
+    uint32_t tie = equal + before.x, stay = 0;
+#pragma unroll
+    for (int e = 0; e < kRowsPerThread; ++e) {
+      const int row = first + e;
+      bool in = row < len && (row < lo || row >= hi);
+      if (!none && row >= lo && row < hi) {
+        if (key[e] == prefix) in = tie++ < need;
+        else in = key[e] > prefix;
+      }
+      stay |= in ? 1u << e : 0u;
+    }
+    equal += total.x;
+    const uint2 at0 = block_scan_two(make_uint2(static_cast<uint32_t>(__popc(stay)), 0u), s_wave, &total);
+    uint32_t at = taken + at0.x;
+#pragma unroll
+    for (int e = 0; e < kRowsPerThread; ++e)
+      if (stay >> e & 1u) {
+        if (at < static_cast<uint32_t>(a.budget)) kept[at] = first + e;
+        ++at;
+      }
+    taken += total.x;
+  }
+  if (w_out == nullptr) return;
+  // the kept rows' weights; in place too, since a row only moves towards the front: a block of them is read before it is written
+  __syncthreads();
+  for (int m0 = 0; m0 < stays; m0 += kSelectThreads) {
+    const int m = m0 + tid;
+    const float x = m < stays ? w[kept[m]] : 0.f;
+    __syncthreads();
+    if (m < stays) w_out[m] = x;
+    __syncthreads();
+  }
+}
+
+// ---- rows move: kept[m] of the source's pages to row m of the destination's.
+// In place a workgroup has one (sequence, KV head) and 64 values of the rows of K or of V and goes through the rows in order, a
+// block of them read before it is written (a row only moves towards the front, so nothing is read behind its write).  Into other
+// pages there is no order, and the rows are spread over as many workgroups as there are blocks.
+constexpr int kMoveThreads = 512;
+constexpr int kMoveChunks = 8;                                     // of 16 bytes per thread and block
+constexpr int kMoveRows = kMoveThreads / 8 * kMoveChunks;          // rows of a block
+__global__ __launch_bounds__(kMoveThreads) void evict_move_kernel(EvictArgs a) {
+  const int groups = (a.Dh + 63) / 64;
+  const int unit = blockIdx.x;                                     // K or V, 64 values
+  const bool is_v = unit >= groups;
+  const int group = unit - (is_v ? groups : 0);
+  const int b = blockIdx.z / a.Hkv, g = blockIdx.z - b * a.Hkv;
+  const int tid = threadIdx.x;
+  const int col = group * 8 + (tid & 7);
+  int len = a.len[b];
+  len = len < 0 ? 0 : (len < a.max_len ? len : a.max_len);
+  len = len < a.src.capacity ? len : a.src.capacity;
+  const int stays = len < a.budget ? len : a.budget;
+  if (a.in_place && stays == len) return;
+  const int room = stays < a.dst.capacity ? stays : a.dst.capacity;
+  if (room < stays && tid == 0) report(a.dst, b, TALON_STATUS_BAD_PAGE);
+  const int32_t* const kept = a.kept + (static_cast<size_t>(b) * a.Hkv + g) * a.budget;
+  const uint16_t* const from = static_cast<const uint16_t*>(is_v ? a.src.v : a.src.k);
+  uint16_t* const to = static_cast<uint16_t*>(is_v ? a.dst.v : a.dst.k);
+  for (int m0 = static_cast<int>(blockIdx.y) * kMoveRows; m0 < room; m0 += static_cast<int>(gridDim.y) * kMoveRows) {
+    uint4 v[kMoveChunks];
+    uint32_t dest[kMoveChunks];
+    uint32_t moved = 0;
+#pragma unroll
+    for (int u = 0; u < kMoveChunks; ++u) {
+      const int m = m0 + (tid >> 3) + kMoveThreads / 8 * u;
+      v[u] = make_uint4(0, 0, 0, 0);
+      dest[u] = 0;
+      if (m < room && col * 8 < a.Dh) {
+        const int row = kept[m];
+        if (!(a.in_place && row == m)) {
+          const uint32_t e_from = page_entry(a.src, b, row), e_to = page_entry(a.dst, b, m);
+          if (e_from < a.src.num_pages && e_to < a.dst.num_pages) {
+            v[u] = *reinterpret_cast<const uint4*>(chunk_at(from, row_chunk(a.src, e_from, row, g) + col));
+            dest[u] = row_chunk(a.dst, e_to, m, g) + col;
+            moved |= 1u << u;
+          } else {
+            report(e_from < a.src.num_pages ? a.dst : a.src, b, TALON_STATUS_BAD_PAGE);
+          }
+        }
+      }
+    }
+    if (a.in_place) __syncthreads();
+#pragma unroll
+    for (int u = 0; u < kMoveChunks; ++u)
+      if (moved >> u & 1u) *reinterpret_cast<uint4*>(chunk_at(to, dest[u])) = v[u];
+  }
+}
+
+}  // namespace
+
+hipError_t launch_rotary_store(const RotaryArgs& a, int dtype, hipStream_t s) {
+  // few tokens: one per workgroup, to have all of them at work; many: four, whose angles fill a workgroup's threads
+  const bool four = static_cast<long long>(a.B) * a.N >= 2048 && a.pairs <= 128;
+  const dim3 grid(four ? (a.N + 3) / 4 : a.N, a.B);
+  const size_t lds = static_cast<size_t>(four ? 4 : 1) * a.pairs * sizeof(float2);
+  const bool f16 = dtype == TALON_DTYPE_F16;
+  if (four) {
+    if (f16) hipLaunchKernelGGL((rotary_store_kernel<true, 4>), grid, dim3(256), lds, s, a);
+    else hipLaunchKernelGGL((rotary_store_kernel<false, 4>), grid, dim3(256), lds, s, a);
+  } else {
+    if (f16) hipLaunchKernelGGL((rotary_store_kernel<true, 1>), grid, dim3(256), lds, s, a);
+    else hipLaunchKernelGGL((rotary_store_kernel<false, 1>), grid, dim3(256), lds, s, a);
+  }
+  return hipGetLastError();
+}
+
+hipError_t launch_paged_compact(const CompactArgs& a, hipStream_t s) {
+  hipLaunchKernelGGL(paged_compact_kernel, dim3(2 * ((a.Dh + 63) / 64), a.Hkv, a.B), dim3(256), 0, s, a);
+  return hipGetLastError();
+}
+
+hipError_t launch_paged_evict(const EvictArgs& a, hipStream_t s) {
+  hipLaunchKernelGGL(evict_select_kernel, dim3(a.Hkv, a.B), dim3(kSelectThreads), 0, s, a);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  const int most = a.budget < a.max_len ? a.budget : a.max_len;
+  if (most == 0) return hipSuccess;
+  const int blocks = a.in_place ? 1 : (most + kMoveRows - 1) / kMoveRows < 65535 ? (most + kMoveRows - 1) / kMoveRows : 65535;
+  hipLaunchKernelGGL(evict_move_kernel, dim3(2 * ((a.Dh + 63) / 64), blocks, a.B * a.Hkv), dim3(kMoveThreads), 0, s, a);
+  return hipGetLastError();
+}
+
+}  // namespace talon
