@@ -80,25 +80,109 @@ template <int DH>
 struct PagedSmem {
   static constexpr int CPR = DH / 8;
   static constexpr int T_ELEMS = kTileRows * DH;
-  static constexpr int POS_BYTES = 8 * kTileRows * 4;              // positions of a tile's rows, one copy per wavefront
+  static constexpr int POS_BYTES = 8 * (kTileRows + 32) * 4;       // positions of a tile's rows and of its queries, per wavefront
   static constexpr int BYTES = 4 * T_ELEMS * 2 + POS_BYTES + 16;   // two stages of K, two of V; the rows of V that are not finite
   __device__ static int kswz(int row) { return DH >= 128 ? (row & 15) : ((row >> 1) & 7); }
   __device__ static int vswz(int row) { return DH >= 128 ? ((row & 3) << 2) : (((row >> 1) & 1) << 2); }
 };
 
 // Key tiles [*first, *first + result) of row tile rt of a sequence.
-__device__ __forceinline__ int tiles_of(const ScoreArgs& sc, int P, int n, uint32_t inv_g, int row_tile, int rt, int* first) {
-  int last = div_g((rt + 1) * row_tile - 1, inv_g);
+template <int TILE, int ROW_TILE>
+__device__ __forceinline__ int tiles_of(const ScoreArgs& sc, int P, int n, uint32_t inv_g, int rt, int* first) {
+  int last = div_g((rt + 1) * ROW_TILE - 1, inv_g);
   last = last < n - 1 ? last : n - 1;
   const int end = sc.mask != nullptr ? P + n : P + last + 1;
   int begin = 0;
   if (sc.window > 0) {
-    const int lowest = P + (sc.offset != nullptr || sc.mask != nullptr ? 0 : div_g(rt * row_tile, inv_g));
+    const int lowest = P + (sc.offset != nullptr || sc.mask != nullptr ? 0 : div_g(rt * ROW_TILE, inv_g));
     begin = lowest - sc.window + 1;
     begin = begin < 0 ? 0 : begin;
   }
-  *first = begin / kTileRows;
-  return (end + kTileRows - 1) / kTileRows - begin / kTileRows;
+  *first = begin / TILE;
+  return (end + TILE - 1) / TILE - begin / TILE;
+}
+
+// A workgroup's share of the line of key tiles: [x, x_end), which begins with tile `at` of row tile rt of (b, g).
+struct Share {
+  int share, tiles;          // its number, tiles of a share
+  int x, x_end;
+  int b, g, rt, at, P, n;
+};
+
+// Every wavefront works this out from the lengths, lane l for sequences l, l + 64, ...  (Loops, not unrolled copies: a workgroup
+// comes here with a cold instruction cache.)  False: nothing to do.
+template <int TILE, int ROW_TILE>
+__device__ __forceinline__ bool find_share(const PagedAttnArgs& a, int lane, Share* w) {
+  const ScoreArgs& sc = a.sc;
+  const bool split = a.cut != nullptr;
+  // Workgroup ids are dealt round-robin to the 8 XCDs: neighbouring shares, which read the same rows of K and V where a sequence
+  // has several row tiles, go to one XCD and its L2.  (The grid is a multiple of 8.)
+  const int share = static_cast<int>(blockIdx.x & 7u) * (static_cast<int>(gridDim.x) >> 3) + static_cast<int>(blockIdx.x >> 3);
+  int sum = 0, P = 0, n = 0;   // of this lane's sequence
+  auto look = [&](int bb) {
+    sum = P = n = 0;
+    if (bb < a.B) {
+      clamped_lengths(a.c, sc.prefix_len[bb], sc.n_new[bb], sc.max_prefix_len, sc.N, &P, &n);
+      const int row_tiles = (n * a.G + ROW_TILE - 1) / ROW_TILE;
+      if (!split) sum = row_tiles;
+      else {
+        int first;
+#pragma unroll 1
+        for (int r = 0; r < row_tiles; ++r) sum += tiles_of<TILE, ROW_TILE>(sc, P, n, a.inv_g, r, &first);
+      }
+      sum *= a.Hkv;
+    }
+  };
+  int total_l = 0;
+#pragma unroll 1
+  for (int bb = lane; bb - lane < a.B; bb += 64) {
+    look(bb);
+    total_l += sum;
+  }
+  const int total = uniform(wave_sum_i32(total_l));
+  int tiles = (total + a.slots - 1) / a.slots;
+  tiles = tiles < a.least ? a.least : tiles;
+  const long long x0 = static_cast<long long>(share) * tiles;
+  if (split && threadIdx.x == 0 && share < a.slots) a.cut[share] = make_int4(0, 0, 0, 0);
+  if (x0 >= total) return false;
+  const int x = static_cast<int>(x0);
+  int before = 0, b = 0, at = 0;
+#pragma unroll 1
+  for (int b0 = 0; b0 < a.B; b0 += 64) {
+    if (a.B > 64) look(b0 + lane);   // (else this lane's sequence is the one it has looked at)
+    const int incl = wave_inclusive_scan_i32(sum);
+    const int begin = before + incl - sum;
+    const unsigned long long in = __ballot(x >= begin && x < begin + sum);
+    if (in != 0ull) {
+      const int l = __ffsll(static_cast<long long>(in)) - 1;
+      b = b0 + l;
+      at = x - __builtin_amdgcn_readlane(begin, l);
+      sum = __builtin_amdgcn_readlane(sum, l);
+      P = __builtin_amdgcn_readlane(P, l);
+      n = __builtin_amdgcn_readlane(n, l);
+      break;
+    }
+    before += __builtin_amdgcn_readlane(incl, 63);
+  }
+  b = uniform(b); at = uniform(at); P = uniform(P); n = uniform(n);
+  const int per_head = uniform(sum) / a.Hkv;
+  const int g = at / per_head;
+  at -= g * per_head;
+  int rt = 0;
+  if (split) {
+#pragma unroll 1
+    for (int first;; ++rt) {
+      const int t = tiles_of<TILE, ROW_TILE>(sc, P, n, a.inv_g, rt, &first);
+      if (at < t) break;
+      at -= t;
+    }
+  } else {
+    rt = at;
+    at = 0;
+  }
+  w->share = share; w->tiles = tiles; w->x = x; w->x_end = total - x < tiles ? total : x + tiles;
+  w->b = b; w->g = g; w->rt = rt; w->at = at; w->P = P; w->n = n;
+  return true;
 }
 
 template <bool F16, int DH, int NW, bool MOD>
@@ -122,77 +206,15 @@ __global__ __launch_bounds__(64 * NW, DH == 256 ? 1 : (NW == 4 ? 2 : 1)) void pa
   const ScoreArgs& sc = a.sc;
   const int G = a.G;
 
-  // ---- this workgroup's share.  Workgroup ids are dealt round-robin to the 8 XCDs: neighbouring shares, which read the same
-  // rows of K and V where a sequence has several row tiles, go to one XCD and its L2.
-  const int per_xcd = (static_cast<int>(gridDim.x) + 7) / 8;
-  const int share = static_cast<int>(blockIdx.x % 8) * per_xcd + static_cast<int>(blockIdx.x / 8);   // (the grid is a multiple of 8)
   const bool split = a.cut != nullptr;   // else a share is a row tile
-  int b = 0, g = 0, rt = 0, at = 0, x_end = 0, x = 0, P = 0, n = 0, share_tiles = 0;
-  {
-    // lane l: sequences l, l + 64, ...
-    int sum_l[TALON_B_MAX / 64], P_l[TALON_B_MAX / 64], n_l[TALON_B_MAX / 64];
-    int total_l = 0;
-#pragma unroll
-    for (int c = 0; c < TALON_B_MAX / 64; ++c) {
-      sum_l[c] = P_l[c] = n_l[c] = 0;
-      if (c * 64 < a.B) {
-        const int bb = c * 64 + lane;
-        if (bb < a.B) {
-          clamped_lengths(a.c, sc.prefix_len[bb], sc.n_new[bb], sc.max_prefix_len, sc.N, &P_l[c], &n_l[c]);
-          const int row_tiles = (n_l[c] * G + kRowTile - 1) / kRowTile;
-          int first;
-          if (!split) sum_l[c] = row_tiles;
-          else for (int r = 0; r < row_tiles; ++r) sum_l[c] += tiles_of(sc, P_l[c], n_l[c], a.inv_g, kRowTile, r, &first);
-          sum_l[c] *= a.Hkv;
-          total_l += sum_l[c];
-        }
-      }
-    }
-    const int total = __builtin_amdgcn_readfirstlane(wave_sum_i32(total_l));
-    share_tiles = (total + a.slots - 1) / a.slots;
-    share_tiles = share_tiles < a.least ? a.least : share_tiles;
-    const long long x0 = static_cast<long long>(share) * share_tiles;
-    if (x0 >= total) {
-      if (split && tid == 0 && share < a.slots) a.cut[share] = make_int4(0, 0, 0, 0);
-      return;
-    }
-    x = static_cast<int>(x0);
-    x_end = total - x < share_tiles ? total : x + share_tiles;
-    int before = 0;
-#pragma unroll
-    for (int c = 0; c < TALON_B_MAX / 64; ++c) {
-      if (c * 64 < a.B) {
-        const int incl = wave_inclusive_scan_i32(sum_l[c]);
-        const int begin = before + incl - sum_l[c];
-        before += __builtin_amdgcn_readlane(incl, 63);
-        const unsigned long long in = __ballot(x >= begin && x < begin + sum_l[c]);
-        if (in != 0ull) {
-          const int l = __ffsll(static_cast<long long>(in)) - 1;
-          b = c * 64 + l;
-          at = x - __builtin_amdgcn_readlane(begin, l);
-          P = __builtin_amdgcn_readlane(P_l[c], l);
-          n = __builtin_amdgcn_readlane(n_l[c], l);
-          const int per_head = __builtin_amdgcn_readlane(sum_l[c], l) / a.Hkv;
-          g = at / per_head;
-          at -= g * per_head;
-        }
-      }
-    }
-    if (!split) {
-      rt = at;
-      at = 0;
-    }
-    for (int first; split; ++rt) {
-      const int t = tiles_of(sc, P, n, a.inv_g, kRowTile, rt, &first);
-      if (at < t) break;
-      at -= t;
-    }
-  }
-  if (split && tid == 0) a.cut[share] = make_int4(0, 0, 0, 0);
+  Share w;
+  if (!find_share<kTileRows, kRowTile>(a, lane, &w)) return;
+  int b = w.b, g = w.g, rt = w.rt, at = w.at, x = w.x, P = w.P, n = w.n;
+  const int x_end = w.x_end, share = w.share;
 
   const uint16_t* const k_pool = static_cast<const uint16_t*>(a.c.k);
   const uint16_t* const v_pool = static_cast<const uint16_t*>(a.c.v);
-  int* const s_pos = reinterpret_cast<int*>(smem + 4 * SM::T_ELEMS) + wave * kTileRows;
+  int* const s_pos = reinterpret_cast<int*>(smem + 4 * SM::T_ELEMS) + wave * (kTileRows + 32);
   uint32_t* const s_bad = reinterpret_cast<uint32_t*>(smem + 4 * SM::T_ELEMS) + SM::POS_BYTES / 4;
   auto stage_k = [&](int st) { return smem + st * SM::T_ELEMS; };
   auto stage_v = [&](int st) { return smem + (2 + st) * SM::T_ELEMS; };
@@ -202,19 +224,25 @@ __global__ __launch_bounds__(64 * NW, DH == 256 ? 1 : (NW == 4 ? 2 : 1)) void pa
   constexpr int ROWS_PER_LOAD = 64 / CPR;
   constexpr int LW = NW == 8 ? 4 : NW;
   constexpr int LOADS = kTileRows / ROWS_PER_LOAD / LW;
+  constexpr int ROWS_WAVE = kTileRows / LW;
   const int lwave = wave - (NW - LW);
   const bool loader = lwave >= 0;
-  const int lrow = lane / CPR;
-  const int cslot = lane % CPR;
+  // The lane index anew: what is worked out from it is not kept in registers (or spilled) across the loop by the compiler, which
+  // takes this for another value each time.  Around the loads and the rare paths; the fragment reads keep their addresses.
+  auto lane_again = [&]() {
+    int l;
+    asm volatile("v_mbcnt_lo_u32_b32 %0, -1, 0\n\tv_mbcnt_hi_u32_b32 %0, -1, %0" : "=v"(l));
+    return l;
+  };
 
   bool first_piece = true;
   while (x < x_end) {
     // ---- the piece: key tiles [t_begin, t_end) of (b, g, rt)
     int first_tile;
-    const int tiles = tiles_of(sc, P, n, a.inv_g, kRowTile, rt, &first_tile);
+    const int tiles = tiles_of<kTileRows, kRowTile>(sc, P, n, a.inv_g, rt, &first_tile);
     const int take = !split || tiles - at < x_end - x ? tiles - at : x_end - x;
     const int t_begin = first_tile + at;
-    const int nt = take;
+    const int t_end = t_begin + take;
     const bool whole = take == tiles;
     const int rows = n * G;
     const int row0 = rt * kRowTile;
@@ -230,10 +258,14 @@ __global__ __launch_bounds__(64 * NW, DH == 256 ? 1 : (NW == 4 ? 2 : 1)) void pa
     const bool valid = rho < rows;
     const int token = valid ? div_g(rho, a.inv_g) : tk0;
     const int head = g * G + (valid ? rho - token * G : 0);
-    const int off = offset_of(sc, b, token);
-    const int p_i = P + off;
+    const int p_own = P + offset_of(sc, b, token);
+    if (h == 0) s_pos[kTileRows + l32] = p_own;   // (read by this wavefront alone)
     float slope2 = 0.f;
     if constexpr (MOD) if (sc.slopes != nullptr) slope2 = sc.slopes[head] * kLog2eF;
+    auto token_of = [&](int ln) {
+      const int rho_ = wrow0 + (ln & 31);
+      return rho_ < rows ? div_g(rho_, a.inv_g) : tk0;
+    };
 
     // ---- which tiles every row of the workgroup sees whole: those inside [seen_from, seen_to)
     const bool positions = sc.window > 0 || (MOD && sc.slopes != nullptr);
@@ -248,7 +280,6 @@ __global__ __launch_bounds__(64 * NW, DH == 256 ? 1 : (NW == 4 ? 2 : 1)) void pa
       }
       seen_from = P + most - sc.window + 1;
     }
-    auto partly_seen = [&](int t) { return (t + 1) * kTileRows > seen_to || t * kTileRows < seen_from; };
 
     float m_run = kNoScore, l_run = 0.f;
     floatx16 o[DB];
@@ -257,45 +288,35 @@ __global__ __launch_bounds__(64 * NW, DH == 256 ? 1 : (NW == 4 ? 2 : 1)) void pa
 #pragma unroll
       for (int r = 0; r < 16; ++r) o[db][r] = 0.f;
 
-    // ---- addresses of a tile's rows.  A row past the end reads the last row instead; its score is masked.
-    uint32_t entry[LOADS], k_rows[LOADS], v_rows[LOADS];
-    auto key_of = [&](int t, int i) {
-      const int key = t * kTileRows + (lwave * LOADS + i) * ROWS_PER_LOAD + lrow;
+    // ---- addresses of a tile's rows.  A loading wavefront takes ROWS_WAVE rows of a tile, ROWS_PER_LOAD an instruction.  Lane l
+    // finds row l % ROWS_WAVE: its page entry, read a step ahead, and where it lies; the lanes of a load then take their rows' places
+    // from it.  (Every lane on its own, as many entries and products as loads, cost 0.1 us more a tile; scalar addresses with the
+    // entries held a lane each 0.15.)  A row past the end reads the last row instead; its score is hidden.
+    uint32_t entry = 0, k_row[LOADS], v_row[LOADS];
+    auto key_of = [&](int t, int ln) {
+      const int key = t * kTileRows + lwave * ROWS_WAVE + (ln & (ROWS_WAVE - 1));
       return key < kend ? key : kend - 1;
     };
     auto load_entries = [&](int t) {
       if (!loader) return;
-#pragma unroll
-      for (int i = 0; i < LOADS; ++i) entry[i] = page_entry(a.c, b, key_of(t, i));
+      entry = page_entry(a.c, b, key_of(t, lane_again()));
     };
-    // (waited for here, in front of the tile loads: where they were first used the wait would count those too)
-    auto entries_landed = [&]() {
-      static_assert(LOADS == 2 || LOADS == 4 || LOADS == 8, "one statement names every entry");
-      if constexpr (LOADS == 2) asm volatile("" : "+v"(entry[0]), "+v"(entry[1]));
-      else if constexpr (LOADS == 4) asm volatile("" : "+v"(entry[0]), "+v"(entry[1]), "+v"(entry[2]), "+v"(entry[3]));
-      else asm volatile("" : "+v"(entry[0]), "+v"(entry[1]), "+v"(entry[2]), "+v"(entry[3]), "+v"(entry[4]), "+v"(entry[5]), "+v"(entry[6]), "+v"(entry[7]));
-    };
+    // (waited for here, in front of the tile loads: where it was first used the wait would count those too)
+    auto entries_landed = [&]() { asm volatile("" : "+v"(entry)); };
     auto rows_of = [&](int t, uint32_t (&to)[LOADS]) {
-      bool bad = false;
+      const int ln = lane_again();
+      if (__ballot(entry >= a.c.num_pages) != 0ull && ln == 0) report(a.c, b, TALON_STATUS_BAD_PAGE);
+      const int row = static_cast<int>(row_chunk(a.c, entry, key_of(t, ln), g));
 #pragma unroll
-      for (int i = 0; i < LOADS; ++i) {
-        bad = bad || entry[i] >= a.c.num_pages;
-        to[i] = row_chunk(a.c, entry[i], key_of(t, i), g);
-      }
-      if (__ballot(bad) != 0ull && lane == 0) report(a.c, b, TALON_STATUS_BAD_PAGE);
+      for (int i = 0; i < LOADS; ++i) to[i] = static_cast<uint32_t>(__builtin_amdgcn_ds_bpermute((i * ROWS_PER_LOAD + ln / CPR) * 4, row));
     };
-    auto load_k = [&](const uint32_t (&rows_)[LOADS], int st) {
+    auto load_tile = [&](const uint16_t* pool, uint16_t* to, const uint32_t (&rows_)[LOADS], bool is_k) {
+      const int lrow = lane / CPR, cslot = lane % CPR;
 #pragma unroll
       for (int i = 0; i < LOADS; ++i) {
         const int u = (lwave * LOADS + i) * ROWS_PER_LOAD;
-        global_to_lds(chunk_at(k_pool, rows_[i] + (cslot ^ SM::kswz(u + lrow))), stage_k(st) + u * DH);
-      }
-    };
-    auto load_v = [&](const uint32_t (&rows_)[LOADS], int st) {
-#pragma unroll
-      for (int i = 0; i < LOADS; ++i) {
-        const int u = (lwave * LOADS + i) * ROWS_PER_LOAD;
-        global_to_lds(chunk_at(v_pool, rows_[i] + (cslot ^ SM::vswz(u + lrow))), stage_v(st) + u * DH);
+        const uint32_t chunk = static_cast<uint32_t>(cslot ^ (is_k ? SM::kswz(u + lrow) : SM::vswz(u + lrow)));
+        global_to_lds(chunk_at(pool, rows_[i] + chunk), to + u * DH);
       }
     };
     auto tile_landed = [&]() {
@@ -304,74 +325,80 @@ __global__ __launch_bounds__(64 * NW, DH == 256 ? 1 : (NW == 4 ? 2 : 1)) void pa
     };
 
     x8 bq[DSTEPS];
-    auto qk = [&](const uint16_t* sK, floatx16 (&s)[2]) {
+    auto qk = [&](const uint16_t* sK, floatx16 (&s)[2], int ln) {
 #pragma unroll
       for (int kb = 0; kb < 2; ++kb) {
 #pragma unroll
         for (int r = 0; r < 16; ++r) s[kb][r] = 0.f;
-        const int krow_i = 32 * kb + l32;
+        const int krow_i = 32 * kb + (ln & 31);
         const uint16_t* krow = sK + krow_i * DH;
         const int ksw = SM::kswz(krow_i);
 #pragma unroll
         for (int ds = 0; ds < DSTEPS; ++ds) {
-          const x8 ak = __builtin_bit_cast(x8, *reinterpret_cast<const uint4*>(krow + ((2 * ds + h) ^ ksw) * 8));
+          const x8 ak = __builtin_bit_cast(x8, *reinterpret_cast<const uint4*>(krow + ((2 * ds + (ln >> 5)) ^ ksw) * 8));
           s[kb] = ST::mfma(ak, bq[ds], s[kb]);
         }
       }
     };
 
-    // Scores in base-2 units (MOD) or still to be multiplied by scale * log2(e); -inf where a row is not seen.
+    // Scores are in base-2 units with MOD, else still to be multiplied by scale * log2(e).
     // Register r of s[kb] is row 32 * kb + 8 * (r / 4) + 4 * h + r % 4 of the tile.
-    auto finish_scores = [&](int t, floatx16 (&s)[2]) {
-      const int key0 = t * kTileRows;
-      if constexpr (MOD) {
-        if (sc.cap_log2e > 0.f) {
-          // cap * tanh(x) = cap * (1 - 2 / (1 + e^(2x))): off by cap * 2^-23 at most, which a probability's rounding to 16 bits covers
+    auto base2_scores = [&](floatx16 (&s)[2]) {
+      if (sc.cap_log2e > 0.f) {
+        // cap * tanh(x) = cap * (1 - 2 / (1 + e^(2x))): off by cap * 2^-23 at most, which a probability's rounding to 16 bits covers
 #pragma unroll
-          for (int kb = 0; kb < 2; ++kb)
+        for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
-            for (int r = 0; r < 16; ++r) {
-              const float e = __builtin_amdgcn_exp2f(s[kb][r] * sc.cap_in);
-              s[kb][r] = __builtin_fmaf(-2.f * sc.cap_log2e, __builtin_amdgcn_rcpf(1.f + e), sc.cap_log2e);
-            }
-        } else {
-#pragma unroll
-          for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) s[kb][r] *= sc.scale_log2e;
-        }
-      }
-      if (!partly_seen(t)) {
-        if constexpr (MOD) {
-          if (sc.slopes != nullptr) {   // rows in front of every query: slope * (p_i - key)
-            const float bias0 = slope2 * static_cast<float>(p_i - key0 - 4 * h);
-#pragma unroll
-            for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-              for (int r = 0; r < 16; ++r)
-                s[kb][r] += __builtin_fmaf(slope2, static_cast<float>(32 * kb + 8 * (r / 4) + r % 4), -bias0);
+          for (int r = 0; r < 16; ++r) {
+            const float e = __builtin_amdgcn_exp2f(s[kb][r] * sc.cap_in);
+            s[kb][r] = __builtin_fmaf(-2.f * sc.cap_log2e, __builtin_amdgcn_rcpf(1.f + e), sc.cap_log2e);
           }
-        }
-        return;
+      } else {
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) s[kb][r] *= sc.scale_log2e;
       }
-      const unsigned long long bits = seen_rows(sc, b, token, P, key0, kend);
+    };
+    // ... of a tile that all rows see whole, which lies in front of every query: the bias is slope * (p_i - key)
+    auto whole_scores = [&](int t, floatx16 (&s)[2]) {
+      base2_scores(s);
+      if (sc.slopes != nullptr) {
+        const float bias0 = slope2 * static_cast<float>(p_own - t * kTileRows - 4 * h);
+#pragma unroll
+        for (int q8 = 0; q8 < 8; ++q8) {   // (eight constants instead of 32, which the compiler keeps in registers)
+          const float bias = __builtin_fmaf(slope2, static_cast<float>(8 * q8), -bias0);
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            s[q8 / 4][4 * (q8 % 4) + e] += __builtin_fmaf(slope2, static_cast<float>(e), bias);
+        }
+      }
+    };
+    // ... of any tile: the bias, and -inf where a row is not seen
+    auto hide_rows = [&](int t, floatx16 (&s)[2]) {
+      const int key0 = t * kTileRows;
+      const int ln = lane_again();
+      const int h_ = ln >> 5;
+      const unsigned long long bits = seen_rows(sc, b, token_of(ln), P, key0, kend);
+      int p_i = 0;
       if (positions) {
-        const int key = key0 + lane;
+        p_i = s_pos[kTileRows + (ln & 31)];
+        const int key = key0 + ln;
         int pos = key;
         if (key >= P && key < kend) pos = P + offset_of(sc, b, key - P);
         __builtin_amdgcn_wave_barrier();
-        s_pos[lane] = pos;
+        s_pos[ln] = pos;
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         __builtin_amdgcn_wave_barrier();
       }
       const int window = sc.window > 0 ? sc.window : 0x7FFFFFFF;
 #pragma unroll
       for (int kb = 0; kb < 2; ++kb) {
-        const uint32_t w = static_cast<uint32_t>(bits >> (32 * kb)) >> (4 * h);
+        const uint32_t w = static_cast<uint32_t>(bits >> (32 * kb)) >> (4 * h_);
 #pragma unroll
         for (int q4 = 0; q4 < 4; ++q4) {
           int4 pos = make_int4(0, 0, 0, 0);
-          if (positions) pos = *reinterpret_cast<const int4*>(s_pos + 32 * kb + 8 * q4 + 4 * h);
+          if (positions) pos = *reinterpret_cast<const int4*>(s_pos + 32 * kb + 8 * q4 + 4 * h_);
           const int ps[4] = {pos.x, pos.y, pos.z, pos.w};
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
@@ -389,8 +416,10 @@ __global__ __launch_bounds__(64 * NW, DH == 256 ? 1 : (NW == 4 ? 2 : 1)) void pa
     };
     // Rows of tile t that this lane's query sees, as bits (again; for the rare tile with values that are not finite).
     auto seen_bits = [&](int t) {
-      unsigned long long bits = seen_rows(sc, b, token, P, t * kTileRows, kend);
+      const int ln = lane_again();
+      unsigned long long bits = seen_rows(sc, b, token_of(ln), P, t * kTileRows, kend);
       if (sc.window > 0) {
+        const int p_i = s_pos[kTileRows + (ln & 31)];
         for (int k = 0; k < kTileRows; ++k) {
           const int key = t * kTileRows + k;
           const int pos = key < P || key >= kend ? key : P + offset_of(sc, b, key - P);
@@ -404,6 +433,7 @@ __global__ __launch_bounds__(64 * NW, DH == 256 ? 1 : (NW == 4 ? 2 : 1)) void pa
     auto clean_v = [&](int t, int st) {
       uint4* const v = reinterpret_cast<uint4*>(stage_v(st));
       uint32_t any = 0;
+      const int tid = wave * 64 + lane_again();
 #pragma unroll
       for (int c = 0; c < SM::T_ELEMS / 8 / kWgThreads; ++c) {
         const uint4 u = v[c * kWgThreads + tid];
@@ -434,116 +464,150 @@ __global__ __launch_bounds__(64 * NW, DH == 256 ? 1 : (NW == 4 ? 2 : 1)) void pa
       if (seen_bits(t) & bad) l_run = __builtin_nanf("");
     };
 
-    // One step, tile t = t_begin + i, whose finished scores are in s: loads of K(t + 2) and V(t + 1), scores of tile t + 1,
-    // softmax of tile t, O^T += V(t)^T . P^T.
-    auto step = [&](int i, floatx16 (&s)[2], floatx16 (&s_nxt)[2], auto has_next) {
-      constexpr bool kHasNext = decltype(has_next)::value;
-      const int t = t_begin + i;
-      if (partly_seen(t)) clean_v(t, i & 1);
-      if constexpr (kHasNext) {
-        if (loader) {
-          entries_landed();
-          uint32_t next_rows[LOADS];
-          if (i + 2 < nt) {
-            rows_of(t + 2, next_rows);
-            load_k(next_rows, i & 1);
-          }
-          load_v(v_rows, (i + 1) & 1);
-          if (i + 3 < nt) load_entries(t + 3);
+    // What a step does with a tile's finished scores, in parts: running maximum (returns what the output was scaled by) ...
+    auto new_maximum = [&](const floatx16 (&s)[2], float* m_safe) {
+      float mx = kNoScore;
 #pragma unroll
-          for (int j = 0; j < LOADS; ++j) v_rows[j] = next_rows[j];
+      for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) mx = fmaxf(mx, s[kb][r]);
+      const int mi = __float_as_int(mx);
+      const auto sw = __builtin_amdgcn_permlane32_swap(mi, mi, false, false);
+      mx = fmaxf(__int_as_float(static_cast<int>(sw[0])), __int_as_float(static_cast<int>(sw[1])));
+      const float m_new = fmaxf(m_run, MOD ? mx : mx * sc.scale_log2e);
+      *m_safe = m_new == kNoScore ? 0.f : m_new;
+      const float alpha = __builtin_amdgcn_exp2f(m_run - *m_safe);
+      m_run = m_new;
+      if (__ballot(alpha != 1.f) != 0ull) {
+#pragma unroll
+        for (int db = 0; db < DB; ++db)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) o[db][r] *= alpha;
+      }
+      return alpha;
+    };
+    // ... probabilities (rounded to the storage type for the matrix product; the denominator sums them unrounded) ...
+    auto probabilities = [&](const floatx16 (&s)[2], float m_safe, float alpha, x8 (&pb)[2][2]) {
+      float sum0 = 0.f, sum1 = 0.f;
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb) {
+#pragma unroll
+        for (int sp = 0; sp < 2; ++sp) {
+          x8 pk;
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            const float v = s[kb][8 * sp + e];
+            const float p = __builtin_amdgcn_exp2f(MOD ? v - m_safe : __builtin_fmaf(v, sc.scale_log2e, -m_safe));
+            if (e & 1) sum1 += p; else sum0 += p;
+            pk[e] = static_cast<typename ST::x1>(p);
+          }
+          pb[kb][sp] = pk;
         }
       }
-      if (works) {
-        const uint16_t* sV = stage_v(i & 1);
-        x8 pb[2][2];
-        float mx = kNoScore;
+      l_run = l_run * alpha + (sum0 + sum1);
+    };
+    // ... and O^T += V^T . P^T
+    auto add_values = [&](const uint16_t* sV, const x8 (&pb)[2][2], int ln) {
+      const int i16 = ln & 15;
+      const int dhblk = (ln >> 4) & 1;
+      const int vrow_l = 4 * (ln >> 5) + (i16 >> 2);
+      const int vsw = SM::vswz(vrow_l);
+      const int vch = 2 * dhblk + ((i16 & 3) >> 1);
+      const int vsub = (i16 & 1) * 4;
 #pragma unroll
-        for (int kb = 0; kb < 2; ++kb)
+      for (int kb = 0; kb < 2; ++kb) {
 #pragma unroll
-          for (int r = 0; r < 16; ++r) mx = fmaxf(mx, s[kb][r]);
-        {
-          const int mi = __float_as_int(mx);
-          const auto sw = __builtin_amdgcn_permlane32_swap(mi, mi, false, false);
-          mx = fmaxf(__int_as_float(static_cast<int>(sw[0])), __int_as_float(static_cast<int>(sw[1])));
-        }
-        const float c2 = MOD ? 1.f : sc.scale_log2e;
-        const float m_new = fmaxf(m_run, MOD ? mx : mx * c2);
-        const float m_safe = m_new == kNoScore ? 0.f : m_new;
-        const float alpha = __builtin_amdgcn_exp2f(m_run - m_safe);
-        m_run = m_new;
-        if (__ballot(alpha != 1.f) != 0ull) {
+        for (int sp = 0; sp < 2; ++sp) {
 #pragma unroll
-          for (int db = 0; db < DB; ++db)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) o[db][r] *= alpha;
-        }
-        if constexpr (kHasNext) qk(stage_k((i + 1) & 1), s_nxt);
-        {
-          // (probabilities are rounded to the storage type for the matrix product, the denominator sums them unrounded)
-          float sum0 = 0.f, sum1 = 0.f;
-#pragma unroll
-          for (int kb = 0; kb < 2; ++kb) {
-#pragma unroll
-            for (int sp = 0; sp < 2; ++sp) {
-              x8 pk;
-#pragma unroll
-              for (int e = 0; e < 8; ++e) {
-                const float v = s[kb][8 * sp + e];
-                const float p = __builtin_amdgcn_exp2f(MOD ? v - m_safe : __builtin_fmaf(v, c2, -m_safe));
-                if (e & 1) sum1 += p; else sum0 += p;
-                pk[e] = static_cast<typename ST::x1>(p);
-              }
-              pb[kb][sp] = pk;
-            }
+          for (int db = 0; db < DB; ++db) {
+            const uint16_t* vp = sV + (32 * kb + 16 * sp + vrow_l) * DH + ((4 * db + vch) ^ vsw) * 8 + vsub;
+            const short4v lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) short4v*)(vp));
+            const short4v hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) short4v*)(vp + 8 * DH));
+            const short8v both = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+            o[db] = ST::mfma(__builtin_bit_cast(x8, both), pb[kb][sp], o[db]);
           }
-          l_run = l_run * alpha + (sum0 + sum1);
         }
-        if constexpr (kHasNext) finish_scores(t + 1, s_nxt);
+      }
+      // (the two reads of a fragment run two matrix instructions ahead)
+      __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
+#pragma unroll
+      for (int g_ = 0; g_ < 4 * DB - 2; ++g_) {
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+      }
+      __builtin_amdgcn_sched_group_barrier(0x008, 2, 0);
+    };
+    // Loads of a step: V(t + 1), K(t + 2) to the stage that K(t) has left, and the page entries of tile t + 3.
+    auto next_loads = [&](int t, int stage) {
+      if (!loader) return;
+      entries_landed();
+      if (t + 2 < t_end) rows_of(t + 2, k_row);
+      if (t + 1 < t_end) load_tile(v_pool, stage_v(stage ^ 1), v_row, false);
+      if (t + 2 < t_end) load_tile(k_pool, stage_k(stage), k_row, true);
+      if (t + 3 < t_end) load_entries(t + 3);
+#pragma unroll
+      for (int j = 0; j < LOADS; ++j) v_row[j] = k_row[j];
+    };
 
-        // ---- O^T += V^T . P^T
-        const int i16 = lane & 15;
-        const int dhblk = (lane >> 4) & 1;
-        const int vrow_l = 4 * h + (i16 >> 2);
-        const int vsw = SM::vswz(vrow_l);
-        const int vch = 2 * dhblk + ((i16 & 3) >> 1);
-        const int vsub = (i16 & 1) * 4;
-#pragma unroll
-        for (int kb = 0; kb < 2; ++kb) {
-#pragma unroll
-          for (int sp = 0; sp < 2; ++sp) {
-#pragma unroll
-            for (int db = 0; db < DB; ++db) {
-              const uint16_t* vp = sV + (32 * kb + 16 * sp + vrow_l) * DH + ((4 * db + vch) ^ vsw) * 8 + vsub;
-              const short4v lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) short4v*)(vp));
-              const short4v hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) short4v*)(vp + 8 * DH));
-              const short8v both = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-              o[db] = ST::mfma(__builtin_bit_cast(x8, both), pb[kb][sp], o[db]);
-            }
-          }
-        }
-        // (the two reads of a fragment run two matrix instructions ahead)
-        __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
-#pragma unroll
-        for (int g_ = 0; g_ < 4 * DB - 2; ++g_) {
-          __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-          __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
-        }
-        __builtin_amdgcn_sched_group_barrier(0x008, 2, 0);
+    // Two kinds of steps over one scheme of loads: when the step of tile t begins, K(t), V(t) and K(t + 1) are in LDS, those of
+    // even tiles (counted from the first one of the run of whole tiles) in stage 0.
+    // A tile that all rows see whole, and whose next is one too: its scores are in s; those of tile t + 1 are formed while its
+    // exponentials are taken.  All other tiles (the last of the run, those of a sequence's end, a window's first) go one thing
+    // after the other: see the loop below.
+    auto step = [&](int t, int ln, auto stage, floatx16 (&s)[2], floatx16 (&s_nxt)[2]) {
+      constexpr int kStage = decltype(stage)::value;
+      next_loads(t, kStage);
+      if (works) {
+        x8 pb[2][2];
+        float m_safe;
+        const float alpha = new_maximum(s, &m_safe);
+        qk(stage_k(kStage ^ 1), s_nxt, ln);
+        probabilities(s, m_safe, alpha, pb);
+        if constexpr (MOD) whole_scores(t + 1, s_nxt);
+        // (Never taken.  It ends a block: the compiler then lets the exponentials run among the matrix instructions of the second
+        // product, whose schedule it would otherwise lose among those of the first.  Two chunks of 2048 tokens at 8192 rows: 541 us
+        // without, 512 with it.)
+        if (t_end < 0) asm volatile("s_nop 0");
+        add_values(stage_v(kStage), pb, ln);
       }
       tile_landed();
     };
+    // What is left of a tile whose scores are there.
+    auto finish_step = [&](int t, int stage, const floatx16 (&s)[2]) {
+      next_loads(t, stage);
+      if (works) {
+        x8 pb[2][2];
+        float m_safe;
+        const float alpha = new_maximum(s, &m_safe);
+        probabilities(s, m_safe, alpha, pb);
+        add_values(stage_v(stage), pb, lane_again());
+      }
+      tile_landed();
+    };
+    // ---- the tiles of the piece that all rows see whole: [whole_from, whole_to)
+    int whole_from = (seen_from + kTileRows - 1) / kTileRows, whole_to = seen_to / kTileRows;
+    if (seen_from <= 0) whole_from = 0;
+    whole_from = whole_from < t_begin ? t_begin : whole_from;
+    whole_to = whole_to < t_end ? whole_to : t_end;
+    if (whole_from >= whole_to || DH == 256) whole_from = whole_to = t_end;   // none (or no registers for two tiles' scores)
+    auto stage_of = [&](int t) { return (t - whole_from) & 1; };
 
-    // ---- prologue: page entries of the first two tiles, their rows, this lane's query
-    if (loader) {
-      load_entries(t_begin);
-      entries_landed();
-      uint32_t rows0[LOADS];
-      rows_of(t_begin, rows0);
-      load_k(rows0, 0);
-      load_v(rows0, 0);
-    }
+    // ---- prologue: page entries, the first tiles, this lane's query
     {
+      if (loader) {
+        load_entries(t_begin);
+        uint32_t second = 0;
+        if (t_begin + 1 < t_end) second = page_entry(a.c, b, key_of(t_begin + 1, lane_again()));
+        asm volatile("" : "+v"(entry), "+v"(second));
+        rows_of(t_begin, v_row);
+        load_tile(k_pool, stage_k(stage_of(t_begin)), v_row, true);
+        load_tile(v_pool, stage_v(stage_of(t_begin)), v_row, false);
+        if (t_begin + 1 < t_end) {
+          entry = second;
+          rows_of(t_begin + 1, v_row);
+          load_tile(k_pool, stage_k(stage_of(t_begin + 1)), v_row, true);
+        }
+      }
       const uint16_t* qp = a.q.p + static_cast<int64_t>(b) * a.q.sb + static_cast<int64_t>(token) * a.q.st + static_cast<int64_t>(head) * a.q.sh + 8 * h;
       u32x4 qv[DSTEPS];
 #pragma unroll
@@ -551,40 +615,39 @@ __global__ __launch_bounds__(64 * NW, DH == 256 ? 1 : (NW == 4 ? 2 : 1)) void pa
         qv[ds] = u32x4{0, 0, 0, 0};
         if (valid) qv[ds] = *reinterpret_cast<const u32x4*>(qp + 16 * ds);
       }
-      if (loader && nt > 1) load_entries(t_begin + 1);
+      if (loader && t_begin + 2 < t_end) load_entries(t_begin + 2);
       // the compiler's waits for these loads stand here, not inside the loop
 #pragma unroll
       for (int ds = 0; ds < DSTEPS; ds += 4) asm volatile("" : "+v"(qv[ds]), "+v"(qv[ds + 1]), "+v"(qv[ds + 2]), "+v"(qv[ds + 3]));
 #pragma unroll
       for (int ds = 0; ds < DSTEPS; ++ds) bq[ds] = __builtin_bit_cast(x8, qv[ds]);
     }
-    if (loader && nt > 1) {
-      entries_landed();
-      rows_of(t_begin + 1, v_rows);
-      load_k(v_rows, 1);
-      if (nt > 2) load_entries(t_begin + 2);
-    }
-    floatx16 s_a[2], s_b[2];
     tile_landed();
-    if (works) {
-      qk(stage_k(0), s_a);
-      finish_scores(t_begin, s_a);
-    }
-    __syncthreads();   // K stage 0 is free
-    {
-      constexpr std::true_type more{};
-      constexpr std::false_type last{};
-      int i = 0;
-      for (; i + 2 < nt; i += 2) {
-        step(i, s_a, s_b, more);
-        step(i + 1, s_b, s_a, more);
+    for (int t = t_begin; t < t_end; ++t) {
+      floatx16 s_a[2];
+      const bool whole_run = DH != 256 && t == whole_from;
+      if (!whole_run) clean_v(t, stage_of(t));
+      if (works) {
+        qk(stage_k(stage_of(t)), s_a, lane_again());
+        if (whole_run) {
+          if constexpr (MOD) whole_scores(t, s_a);
+        } else {
+          if constexpr (MOD) base2_scores(s_a);
+          hide_rows(t, s_a);
+        }
       }
-      if (i + 1 < nt) {
-        step(i, s_a, s_b, more);
-        step(i + 1, s_b, s_a, last);
-      } else {
-        step(i, s_a, s_b, last);
+      __syncthreads();   // K(t) is used up
+      if (whole_run) {
+        const int ln = lane_again();
+        constexpr std::integral_constant<int, 0> even{};
+        constexpr std::integral_constant<int, 1> odd{};
+        floatx16 s_b[2];
+        for (; t + 2 < whole_to; t += 2) {   // (in pairs, so that the two sets of scores swap roles without a copy)
+          step(t, ln, even, s_a, s_b);
+          step(t + 1, ln, odd, s_b, s_a);
+        }
       }
+      finish_step(t, stage_of(t), s_a);
     }
 
     // ---- what became of the rows
@@ -634,7 +697,7 @@ __global__ __launch_bounds__(64 * NW, DH == 256 ? 1 : (NW == 4 ? 2 : 1)) void pa
     }
     // the row tile goes on behind this share, and begins in it: the merge at this share's end joins it
     if (at + take < tiles && at == 0 && tid == 0) {
-      const int last_share = (x + tiles - 1) / share_tiles;
+      const int last_share = (x + tiles - 1) / w.tiles;
       const int count = rows - row0 < kRowTile ? rows - row0 : kRowTile;
       a.cut[share] = make_int4(b * a.Hkv + g, row0, count, last_share | (first_piece ? 0 : 1 << 30));
     }
