@@ -176,8 +176,12 @@ int talon_paged_attention(const talon_paged_cache* cache, const talon_view* q, i
     a.cut = reinterpret_cast<int4*>(w + p.off_cut);
   }
   const hipStream_t s = static_cast<hipStream_t>(stream);
-  return check_hip(cache->dtype == TALON_DTYPE_F16 ? launch_paged_attention_f16(a, Dh, p.waves, s) : launch_paged_attention_bf16(a, Dh, p.waves, s),
-                   "paged attention launch");
+  const bool f16 = cache->dtype == TALON_DTYPE_F16;
+  hipError_t e;
+  if (Dh == 64) e = f16 ? launch_paged_attention_f16_64(a, p.waves, s) : launch_paged_attention_bf16_64(a, p.waves, s);
+  else if (Dh == 128) e = f16 ? launch_paged_attention_f16_128(a, p.waves, s) : launch_paged_attention_bf16_128(a, p.waves, s);
+  else e = f16 ? launch_paged_attention_f16_256(a, p.waves, s) : launch_paged_attention_bf16_256(a, p.waves, s);
+  return check_hip(e, "paged attention launch");
 }
 
 int talon_paged_weights(const talon_paged_cache* cache, const talon_view* q, int32_t N, int32_t Hq, const int32_t* n_new,

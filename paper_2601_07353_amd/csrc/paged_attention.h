@@ -1,5 +1,5 @@
 // Attention of new tokens over a paged cache (App. B's tree attention where the cache is kept in pages), included by one
-// source per storage type.
+// source per storage type and head width.
 //
 //   x_ij = scale q_i . k_j,   capped: cap tanh(x / cap),   biased: - slope_h |p_i - p_j|,   -inf where i does not see j
 //   out_i = sum_j softmax_j(x_ij) v_j,   lse_i = log sum_j exp(x_ij)
@@ -185,8 +185,9 @@ __device__ __forceinline__ bool find_share(const PagedAttnArgs& a, int lane, Sha
   return true;
 }
 
-template <bool F16, int DH, int NW, bool MOD>
+template <bool F16, int DH, int NW, bool CAP, bool BIAS>
 __global__ __launch_bounds__(64 * NW, DH == 256 ? 1 : (NW == 4 ? 2 : 1)) void paged_attention_kernel(PagedAttnArgs a) {
+  constexpr bool MOD = CAP || BIAS;   // scores are brought to base-2 units before the softmax
   using ST = Storage<F16>;
   using x8 = typename ST::x8;
   using x4 = typename ST::x4;
@@ -261,14 +262,14 @@ __global__ __launch_bounds__(64 * NW, DH == 256 ? 1 : (NW == 4 ? 2 : 1)) void pa
     const int p_own = P + offset_of(sc, b, token);
     if (h == 0) s_pos[kTileRows + l32] = p_own;   // (read by this wavefront alone)
     float slope2 = 0.f;
-    if constexpr (MOD) if (sc.slopes != nullptr) slope2 = sc.slopes[head] * kLog2eF;
+    if constexpr (BIAS) slope2 = sc.slopes[head] * kLog2eF;
     auto token_of = [&](int ln) {
       const int rho_ = wrow0 + (ln & 31);
       return rho_ < rows ? div_g(rho_, a.inv_g) : tk0;
     };
 
     // ---- which tiles every row of the workgroup sees whole: those inside [seen_from, seen_to)
-    const bool positions = sc.window > 0 || (MOD && sc.slopes != nullptr);
+    const bool positions = sc.window > 0 || BIAS;
     int seen_to = sc.mask != nullptr || (positions && sc.offset != nullptr) ? P : P + tk0 + 1;
     int seen_from = 0;
     if (sc.window > 0) {
@@ -339,12 +340,20 @@ __global__ __launch_bounds__(64 * NW, DH == 256 ? 1 : (NW == 4 ? 2 : 1)) void pa
           s[kb] = ST::mfma(ak, bq[ds], s[kb]);
         }
       }
+      // (fragments are read four matrix instructions ahead)
+      __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
+#pragma unroll
+      for (int g_ = 0; g_ < 2 * DSTEPS - 4; ++g_) {
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+      }
+      __builtin_amdgcn_sched_group_barrier(0x008, 4, 0);
     };
 
     // Scores are in base-2 units with MOD, else still to be multiplied by scale * log2(e).
     // Register r of s[kb] is row 32 * kb + 8 * (r / 4) + 4 * h + r % 4 of the tile.
     auto base2_scores = [&](floatx16 (&s)[2]) {
-      if (sc.cap_log2e > 0.f) {
+      if constexpr (CAP) {
         // cap * tanh(x) = cap * (1 - 2 / (1 + e^(2x))): off by cap * 2^-23 at most, which a probability's rounding to 16 bits covers
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb)
@@ -363,7 +372,7 @@ __global__ __launch_bounds__(64 * NW, DH == 256 ? 1 : (NW == 4 ? 2 : 1)) void pa
     // ... of a tile that all rows see whole, which lies in front of every query: the bias is slope * (p_i - key)
     auto whole_scores = [&](int t, floatx16 (&s)[2]) {
       base2_scores(s);
-      if (sc.slopes != nullptr) {
+      if constexpr (BIAS) {
         const float bias0 = slope2 * static_cast<float>(p_own - t * kTileRows - 4 * h);
 #pragma unroll
         for (int q8 = 0; q8 < 8; ++q8) {   // (eight constants instead of 32, which the compiler keeps in registers)
@@ -407,7 +416,7 @@ __global__ __launch_bounds__(64 * NW, DH == 256 ? 1 : (NW == 4 ? 2 : 1)) void pa
             if (positions) {
               const int apart = p_i - ps[e];
               seen = seen && apart < window;
-              if constexpr (MOD) s[kb][r] = __builtin_fmaf(-slope2, fabsf(static_cast<float>(apart)), s[kb][r]);
+              if constexpr (BIAS) s[kb][r] = __builtin_fmaf(-slope2, fabsf(static_cast<float>(apart)), s[kb][r]);
             }
             s[kb][r] = seen ? s[kb][r] : kNoScore;
           }
@@ -563,11 +572,11 @@ __global__ __launch_bounds__(64 * NW, DH == 256 ? 1 : (NW == 4 ? 2 : 1)) void pa
         const float alpha = new_maximum(s, &m_safe);
         qk(stage_k(kStage ^ 1), s_nxt, ln);
         probabilities(s, m_safe, alpha, pb);
-        if constexpr (MOD) whole_scores(t + 1, s_nxt);
         // (Never taken.  It ends a block: the compiler then lets the exponentials run among the matrix instructions of the second
         // product, whose schedule it would otherwise lose among those of the first.  Two chunks of 2048 tokens at 8192 rows: 541 us
         // without, 512 with it.)
         if (t_end < 0) asm volatile("s_nop 0");
+        if constexpr (MOD) whole_scores(t + 1, s_nxt);   // (among the matrix instructions of the second product)
         add_values(stage_v(kStage), pb, ln);
       }
       tile_landed();
@@ -808,36 +817,37 @@ __global__ __launch_bounds__(256) void paged_attention_join_kernel(PagedAttnArgs
   }
 }
 
-template <bool F16, int DH, int NW, bool MOD>
-hipError_t launch_paged_one(const PagedAttnArgs& a, hipStream_t s) {
-  auto kern = paged_attention_kernel<F16, DH, NW, MOD>;
-  static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize,
-                                                     PagedSmem<DH>::BYTES);
-  if (attr != hipSuccess) return attr;
-  hipLaunchKernelGGL(kern, dim3((a.slots + 7) / 8 * 8), dim3(64 * NW), PagedSmem<DH>::BYTES, s, a);
-  hipError_t e = hipGetLastError();
-  if (e != hipSuccess || a.cut == nullptr) return e;
+template <bool F16, int DH>
+hipError_t launch_paged_join(const PagedAttnArgs& a, hipStream_t s) {
   constexpr int RPW = 256 / (DH / 4);
   hipLaunchKernelGGL((paged_attention_join_kernel<F16, DH>), dim3((a.rows_slot + RPW - 1) / RPW, a.slots), dim3(256), 0, s, a);
   return hipGetLastError();
 }
 
-template <bool F16, int DH>
-hipError_t launch_paged_dh(const PagedAttnArgs& a, int waves, hipStream_t s) {
-  const bool mod = a.sc.cap_log2e > 0.f || a.sc.slopes != nullptr;
-  if constexpr (DH != 256) {
-    if (waves == 8) return mod ? launch_paged_one<F16, DH, 8, true>(a, s) : launch_paged_one<F16, DH, 8, false>(a, s);
-  }
-  return mod ? launch_paged_one<F16, DH, 4, true>(a, s) : launch_paged_one<F16, DH, 4, false>(a, s);
+template <bool F16, int DH, int NW, bool CAP, bool BIAS>
+hipError_t launch_paged_one(const PagedAttnArgs& a, hipStream_t s) {
+  auto kern = paged_attention_kernel<F16, DH, NW, CAP, BIAS>;
+  static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize,
+                                                     PagedSmem<DH>::BYTES);
+  if (attr != hipSuccess) return attr;
+  hipLaunchKernelGGL(kern, dim3((a.slots + 7) / 8 * 8), dim3(64 * NW), PagedSmem<DH>::BYTES, s, a);
+  hipError_t e = hipGetLastError();
+  return e != hipSuccess || a.cut == nullptr ? e : launch_paged_join<F16, DH>(a, s);
 }
 
-template <bool F16>
-hipError_t launch_paged(const PagedAttnArgs& a, int Dh, int waves, hipStream_t s) {
-  switch (Dh) {
-    case 64: return launch_paged_dh<F16, 64>(a, waves, s);
-    case 128: return launch_paged_dh<F16, 128>(a, waves, s);
-    default: return launch_paged_dh<F16, 256>(a, waves, s);
+template <bool F16, int DH, int NW>
+hipError_t launch_paged_waves(const PagedAttnArgs& a, hipStream_t s) {
+  if (a.sc.cap_log2e > 0.f)
+    return a.sc.slopes != nullptr ? launch_paged_one<F16, DH, NW, true, true>(a, s) : launch_paged_one<F16, DH, NW, true, false>(a, s);
+  return a.sc.slopes != nullptr ? launch_paged_one<F16, DH, NW, false, true>(a, s) : launch_paged_one<F16, DH, NW, false, false>(a, s);
+}
+
+template <bool F16, int DH>
+hipError_t launch_paged(const PagedAttnArgs& a, int waves, hipStream_t s) {
+  if constexpr (DH != 256) {   // (heads of 256 leave no registers for two wavefronts on a SIMD)
+    if (waves == 8) return launch_paged_waves<F16, DH, 8>(a, s);
   }
+  return launch_paged_waves<F16, DH, 4>(a, s);
 }
 
 }  // namespace

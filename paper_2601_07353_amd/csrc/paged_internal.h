@@ -105,8 +105,12 @@ struct CompactArgs {
   int B, N, Hkv, Dh;
 };
 
-hipError_t launch_paged_attention_bf16(const PagedAttnArgs& a, int Dh, int waves, hipStream_t s);
-hipError_t launch_paged_attention_f16(const PagedAttnArgs& a, int Dh, int waves, hipStream_t s);
+hipError_t launch_paged_attention_bf16_64(const PagedAttnArgs& a, int waves, hipStream_t s);
+hipError_t launch_paged_attention_bf16_128(const PagedAttnArgs& a, int waves, hipStream_t s);
+hipError_t launch_paged_attention_bf16_256(const PagedAttnArgs& a, int waves, hipStream_t s);
+hipError_t launch_paged_attention_f16_64(const PagedAttnArgs& a, int waves, hipStream_t s);
+hipError_t launch_paged_attention_f16_128(const PagedAttnArgs& a, int waves, hipStream_t s);
+hipError_t launch_paged_attention_f16_256(const PagedAttnArgs& a, int waves, hipStream_t s);
 hipError_t launch_paged_weights(const PagedWeightArgs& a, int Dh, int dtype, hipStream_t s);
 hipError_t launch_rotary_store(const RotaryArgs& a, int dtype, hipStream_t s);
 hipError_t launch_paged_evict(const EvictArgs& a, hipStream_t s);

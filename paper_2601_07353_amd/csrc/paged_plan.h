@@ -7,7 +7,7 @@
 namespace talon {
 
 struct PagedPlan {
-  int waves;        // wavefronts per workgroup
+  int waves;        // wavefronts per workgroup that has rows for each; 0: few rows, the wavefronts share the keys
   int split;        // 1: row tiles are cut into shares; 0: a workgroup per row tile, nothing to join
   int slots;        // workgroups
   int least;        // fewest key tiles of a share
@@ -19,25 +19,30 @@ struct PagedPlan {
 constexpr int kPagedTile = 64;
 constexpr int kPagedWholeTiles = 4;   // up to so many key tiles a row tile is not cut
 constexpr int kPagedLeast = 2;        // fewest key tiles of a share
+constexpr int kPagedFewTile = 32;     // the same for few rows
+constexpr int kPagedFewWhole = 32;
+constexpr int kPagedFewLeast = 8;
 
 inline PagedPlan paged_plan(int B, int N, int Hq, int Hkv, int Dh, int max_prefix_len) {
   PagedPlan p = {};
   const long long rows = static_cast<long long>(N) * (Hq / Hkv);
-  p.waves = Dh != 256 && rows >= 512 ? 8 : 4;
-  const int row_tile = 32 * p.waves;
+  const bool few = rows <= 32;
+  p.waves = few ? 0 : (Dh != 256 && rows >= 512 ? 8 : 4);
+  const int row_tile = few ? 32 : 32 * p.waves;
+  const int tile = few ? kPagedFewTile : kPagedTile;
   const long long items = static_cast<long long>(B) * Hkv * ((rows + row_tile - 1) / row_tile);
-  const long long most = (static_cast<long long>(max_prefix_len) + N + kPagedTile - 1) / kPagedTile;
+  const long long most = (static_cast<long long>(max_prefix_len) + N + tile - 1) / tile;
   p.tiles = items * most;
   p.rows_slot = static_cast<int>(rows < row_tile ? rows : row_tile);
-  p.split = most > kPagedWholeTiles ? 1 : 0;
+  p.split = most > (few ? kPagedFewWhole : kPagedWholeTiles) ? 1 : 0;
   if (!p.split) {
     p.slots = static_cast<int>(items < (1ll << 30) ? items : (1ll << 30));
     p.least = 1;
     p.bytes = 256;   // nothing is staged, keep a token size
     return p;
   }
-  p.least = kPagedLeast;
-  const long long slots = p.waves == 8 || Dh == 256 ? 256 : 512;   // workgroups that the device holds at once
+  p.least = few ? kPagedFewLeast : kPagedLeast;
+  const long long slots = few ? (Dh == 64 ? 512 : 256) : (p.waves == 8 || Dh == 256 ? 256 : 512);   // workgroups that the device holds at once
   const long long enough = (p.tiles + p.least - 1) / p.least;
   p.slots = static_cast<int>(enough < slots ? enough : slots);
   const size_t slot_rows = 2 * static_cast<size_t>(p.slots) * p.rows_slot;

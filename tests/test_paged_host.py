@@ -129,7 +129,7 @@ def test_what_else_is_refused(lib):
 
 def test_workspace_sizes(lib):
     size = lib.talon_paged_attention_workspace_bytes
-    assert size(1, 1, 32, 8, 128, 100) == 256                     # nothing is cut
+    assert size(1, 1, 32, 8, 128, 1000) == 256 and size(1, 60, 32, 8, 128, 100) == 256                   # nothing is cut
     assert 0 < size(1, 1, 32, 8, 128, 2048) < size(1, 64, 32, 8, 128, 2048) <= size(64, 2048, 32, 8, 128, 8192) < 80 << 20
     for bad in [(0, 1, 8, 8, 128, 0), (1, 0, 8, 8, 128, 0), (1, 1, 8, 0, 128, 0), (1, 1, 0, 8, 128, 0), (1, 1, 8, 8, 96, 0), (1, 1, 8, 8, 128, -1), (1, 1, 9, 8, 128, 0),
                 (256, 65536, 128, 1, 128, 1 << 30)]:
@@ -240,9 +240,9 @@ int main() {
     const PagedPlan p = paged_plan(B, N, G * H, H, D, L);
     if (p.tiles >= 1ll << 30) continue;                       // refused
     ++count;
-    const long long rows = (long long)N * G, tile = 32 * p.waves, items = (long long)B * H * ((rows + tile - 1) / tile);
-    const long long most = ((long long)L + N + 63) / 64;
-    bool ok = p.slots >= 1 && (p.waves == 4 || p.waves == 8) && (D != 256 || p.waves == 4) && p.rows_slot <= tile && p.rows_slot <= rows;
+    const long long rows = (long long)N * G, tile = p.waves ? 32 * p.waves : 32, keys = p.waves ? 64 : 32, items = (long long)B * H * ((rows + tile - 1) / tile);
+    const long long most = ((long long)L + N + keys - 1) / keys;
+    bool ok = p.slots >= 1 && (p.waves == 4 || p.waves == 8 || (p.waves == 0 && rows <= 32)) && (D != 256 || p.waves != 8) && p.rows_slot <= tile && p.rows_slot <= rows;
     if (p.split) {
       long long share = (p.tiles + p.slots - 1) / p.slots;
       if (share < p.least) share = p.least;
@@ -251,7 +251,7 @@ int main() {
       ok = ok && p.off_m >= 2ull * p.slots * p.rows_slot * D * 4 && p.off_l - p.off_m >= 2ull * p.slots * p.rows_slot * 4 &&
            p.off_cut - p.off_l >= 2ull * p.slots * p.rows_slot * 4 && p.bytes - p.off_cut >= 16ull * p.slots && p.off_m % 16 == 0 && p.off_cut % 16 == 0;
     } else {
-      ok = ok && p.slots == items && most <= kPagedWholeTiles;
+      ok = ok && p.slots == items && most <= (p.waves ? kPagedWholeTiles : kPagedFewWhole);
     }
     if (!ok) { ++bad; printf("B=%d N=%d G=%d H=%d D=%d L=%d\n", B, N, G, H, D, L); }
   }
