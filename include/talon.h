@@ -526,7 +526,7 @@ typedef struct talon_view {
  */
 typedef struct talon_scores {
   const uint64_t* mask;     /* NULL: causal                                                      */
-  const int32_t* offset;    /* [B][N], a negative one counts as 0; NULL: i                       */
+  const int32_t* offset;    /* [B][N], between 0 and 2^30 - 1 (else the nearest); NULL: i                     */
   const float* slopes;      /* [Hq] or NULL                                                      */
   float scale;              /* 0: 1/sqrt(Dh)                                                     */
   float softcap;            /* 0: none                                                           */

@@ -165,7 +165,7 @@ int talon_paged_attention(const talon_paged_cache* cache, const talon_view* q, i
   if (p.tiles >= 1ll << 30) { set_error("%lld key tiles are more than one call takes", p.tiles); return TALON_ERR_UNSUPPORTED; }
   a.lse = out_lse;
   a.B = B; a.Hkv = Hkv; a.G = Hq / Hkv; a.inv_g = inverse_of(a.G);
-  a.slots = p.slots; a.least = p.least; a.rows_slot = p.rows_slot;
+  a.slots = p.slots; a.least = p.least; a.extra = p.extra; a.rows_slot = p.rows_slot;
   if (p.split) {
     if (!workspace || !aligned16(workspace)) { set_error("workspace is NULL or not 16-byte aligned"); return TALON_ERR_INVALID_ARG; }
     if (workspace_bytes < p.bytes) { set_error("workspace of %zu bytes is smaller than the %zu needed", workspace_bytes, p.bytes); return TALON_ERR_WORKSPACE; }

@@ -16,13 +16,14 @@
 //
 // Work.  Every (sequence, KV head, row tile) needs a number of key tiles that the host does not know (lengths are on the
 // device).  All of them, end to end in that order, are one line of W tiles, cut into equal shares of ceil(W / workgroups), at
-// least `least`: whatever the lengths are, no workgroup has more than a tile more than another.  A share ends inside a row
+// least `least`: whatever the lengths are, no workgroup has more than a tile more than another.  (In front of a
+// row tile's tiles the line has `extra` units of nothing, for what a workgroup does besides: queries, first loads, outputs.)  A share ends inside a row
 // tile as a rule: what it has of it goes to a slot (output not yet divided, maximum, denominator; fp32), and a second kernel
 // joins the slots of a row tile in the order of the shares.  A row tile that lies in one share is written at once.
 // A share's first incomplete piece lies in slot 2 * share, a last one that is not also its first in 2 * share + 1; cut[share]
 // says what the merge behind the share's end has to do: {sequence * Hkv + KV head, first row, rows, last share | (slot & 1) << 30},
 // rows = 0 where nothing begins to be cut there.  Where every row tile has a few key tiles at most, nothing is cut: a share is
-// a row tile, and there is no second launch.
+// a row tile, and there is no second launch.  Where there is little work, a share is one of the even pieces of a row tile.
 //
 // Values of V that are no finite numbers must not reach a row that does not see them (0 * NaN), so a tile that some row of the
 // workgroup does not see whole is looked through for them first; where there are any they are set to zero and the rows that
@@ -64,6 +65,7 @@ struct Storage {
 };
 
 constexpr int kTileRows = 64;
+constexpr int kMaskWords = 4;   // a mask of up to 256 new tokens is kept in LDS
 
 // 16 bytes per lane from global memory to LDS, lane l at lds_base + 16 * l.  In assembly, because the compiler waits for all
 // outstanding loads of its builtin before any LDS read; the waits are tile_landed()'s.
@@ -81,7 +83,8 @@ struct PagedSmem {
   static constexpr int CPR = DH / 8;
   static constexpr int T_ELEMS = kTileRows * DH;
   static constexpr int POS_BYTES = 8 * (kTileRows + 32) * 4;       // positions of a tile's rows and of its queries, per wavefront
-  static constexpr int BYTES = 4 * T_ELEMS * 2 + POS_BYTES + 16;   // two stages of K, two of V; the rows of V that are not finite
+  static constexpr int MASK_BYTES = 256 * kMaskWords * 8;          // mask words of the queries
+  static constexpr int BYTES = 4 * T_ELEMS * 2 + POS_BYTES + MASK_BYTES + 16;   // two stages of K, two of V; the rows of V that are not finite
   __device__ static int kswz(int row) { return DH >= 128 ? (row & 15) : ((row >> 1) & 7); }
   __device__ static int vswz(int row) { return DH >= 128 ? ((row & 3) << 2) : (((row >> 1) & 1) << 2); }
 };
@@ -102,11 +105,13 @@ __device__ __forceinline__ int tiles_of(const ScoreArgs& sc, int P, int n, uint3
   return (end + TILE - 1) / TILE - begin / TILE;
 }
 
-// A workgroup's share of the line of key tiles: [x, x_end), which begins with tile `at` of row tile rt of (b, g).
+// A workgroup's share of the line of key tiles: [x, x_end), which begins with tile `at` of row tile rt of (b, g).  Or a piece of one
+// row tile, `take` tiles from `at` on, the last one of which has share `last`.
 struct Share {
   int share, tiles;          // its number, tiles of a share
   int x, x_end;
   int b, g, rt, at, P, n;
+  int take, last;            // of a piece (take > 0)
 };
 
 // Every wavefront works this out from the lengths, lane l for sequences l, l + 64, ...  (Loops, not unrolled copies: a workgroup
@@ -118,9 +123,10 @@ __device__ __forceinline__ bool find_share(const PagedAttnArgs& a, int lane, Sha
   // Workgroup ids are dealt round-robin to the 8 XCDs: neighbouring shares, which read the same rows of K and V where a sequence
   // has several row tiles, go to one XCD and its L2.  (The grid is a multiple of 8.)
   const int share = static_cast<int>(blockIdx.x & 7u) * (static_cast<int>(gridDim.x) >> 3) + static_cast<int>(blockIdx.x >> 3);
-  int sum = 0, P = 0, n = 0;   // of this lane's sequence
+  int sum = 0, pieces = 0, P = 0, n = 0;   // of this lane's sequence: its tiles, its pieces of at most `least` tiles
+  auto pieces_of = [&](int tiles) { return (tiles + a.least - 1) / a.least; };
   auto look = [&](int bb) {
-    sum = P = n = 0;
+    sum = pieces = P = n = 0;
     if (bb < a.B) {
       clamped_lengths(a.c, sc.prefix_len[bb], sc.n_new[bb], sc.max_prefix_len, sc.N, &P, &n);
       const int row_tiles = (n * a.G + ROW_TILE - 1) / ROW_TILE;
@@ -128,36 +134,50 @@ __device__ __forceinline__ bool find_share(const PagedAttnArgs& a, int lane, Sha
       else {
         int first;
 #pragma unroll 1
-        for (int r = 0; r < row_tiles; ++r) sum += tiles_of<TILE, ROW_TILE>(sc, P, n, a.inv_g, r, &first);
+        for (int r = 0; r < row_tiles; ++r) {
+          const int tiles = tiles_of<TILE, ROW_TILE>(sc, P, n, a.inv_g, r, &first);
+          sum += tiles + a.extra;
+          pieces += pieces_of(tiles);
+        }
       }
       sum *= a.Hkv;
+      pieces *= a.Hkv;
     }
   };
-  int total_l = 0;
+  int total_l = 0, pieces_l = 0;
 #pragma unroll 1
   for (int bb = lane; bb - lane < a.B; bb += 64) {
     look(bb);
     total_l += sum;
+    pieces_l += pieces;
   }
-  const int total = uniform(wave_sum_i32(total_l));
+  int total = uniform(wave_sum_i32(total_l));   // of tiles and what row tiles cost besides them
   int tiles = (total + a.slots - 1) / a.slots;
-  tiles = tiles < a.least ? a.least : tiles;
+  // Little work: pieces of single row tiles, no share with two of them (and their two prologues)
+  bool alone = false;
+  if (split && tiles <= a.least) {
+    const int all = uniform(wave_sum_i32(pieces_l));
+    alone = all <= a.slots;
+    if (alone) total = all;
+  }
+  tiles = alone ? 1 : (tiles < a.least ? a.least : tiles);
   const long long x0 = static_cast<long long>(share) * tiles;
   if (split && threadIdx.x == 0 && share < a.slots) a.cut[share] = make_int4(0, 0, 0, 0);
   if (x0 >= total) return false;
   const int x = static_cast<int>(x0);
-  int before = 0, b = 0, at = 0;
+  int before = 0, b = 0, at = 0, mine = 0;
 #pragma unroll 1
   for (int b0 = 0; b0 < a.B; b0 += 64) {
     if (a.B > 64) look(b0 + lane);   // (else this lane's sequence is the one it has looked at)
-    const int incl = wave_inclusive_scan_i32(sum);
-    const int begin = before + incl - sum;
-    const unsigned long long in = __ballot(x >= begin && x < begin + sum);
+    const int units = alone ? pieces : sum;
+    const int incl = wave_inclusive_scan_i32(units);
+    const int begin = before + incl - units;
+    const unsigned long long in = __ballot(x >= begin && x < begin + units);
     if (in != 0ull) {
       const int l = __ffsll(static_cast<long long>(in)) - 1;
       b = b0 + l;
       at = x - __builtin_amdgcn_readlane(begin, l);
-      sum = __builtin_amdgcn_readlane(sum, l);
+      mine = __builtin_amdgcn_readlane(units, l);
       P = __builtin_amdgcn_readlane(P, l);
       n = __builtin_amdgcn_readlane(n, l);
       break;
@@ -165,16 +185,27 @@ __device__ __forceinline__ bool find_share(const PagedAttnArgs& a, int lane, Sha
     before += __builtin_amdgcn_readlane(incl, 63);
   }
   b = uniform(b); at = uniform(at); P = uniform(P); n = uniform(n);
-  const int per_head = uniform(sum) / a.Hkv;
+  const int per_head = uniform(mine) / a.Hkv;
   const int g = at / per_head;
   at -= g * per_head;
   int rt = 0;
+  w->take = 0;
+  w->last = 0;
   if (split) {
 #pragma unroll 1
     for (int first;; ++rt) {
       const int t = tiles_of<TILE, ROW_TILE>(sc, P, n, a.inv_g, rt, &first);
-      if (at < t) break;
-      at -= t;
+      const int k = alone ? pieces_of(t) : t + a.extra;
+      if (at < k) {
+        if (alone) {   // piece `at` of k even ones
+          w->last = share + k - 1 - at;
+          const int begin = static_cast<int>(static_cast<long long>(t) * at / k);
+          w->take = static_cast<int>(static_cast<long long>(t) * (at + 1) / k) - begin;
+          at = begin;
+        }
+        break;
+      }
+      at -= k;
     }
   } else {
     rt = at;
@@ -183,6 +214,21 @@ __device__ __forceinline__ bool find_share(const PagedAttnArgs& a, int lane, Sha
   w->share = share; w->tiles = tiles; w->x = x; w->x_end = total - x < tiles ? total : x + tiles;
   w->b = b; w->g = g; w->rt = rt; w->at = at; w->P = P; w->n = n;
   return true;
+}
+
+// What a share has of a row tile of `tiles` tiles, from unit `at` of it on.
+struct Piece {
+  int from, to;    // its tiles
+  int units;       // its length on the line
+  int last;        // share of the row tile's last tile
+};
+__device__ __forceinline__ Piece next_piece(const PagedAttnArgs& a, const Share& w, int tiles, int at, int x) {
+  if (a.cut == nullptr) return {0, tiles, 1, 0};
+  if (w.take > 0) return {at, at + w.take, w.x_end - x, w.last};
+  const int rest = tiles + a.extra - at;
+  const int units = rest < w.x_end - x ? rest : w.x_end - x;
+  const int from = at - a.extra, to = at + units - a.extra;
+  return {from < 0 ? 0 : from, to < 0 ? 0 : to, units, (x - at + a.extra + tiles - 1) / w.tiles};
 }
 
 template <bool F16, int DH, int NW, bool CAP, bool BIAS>
@@ -216,7 +262,8 @@ __global__ __launch_bounds__(64 * NW, DH == 256 ? 1 : (NW == 4 ? 2 : 1)) void pa
   const uint16_t* const k_pool = static_cast<const uint16_t*>(a.c.k);
   const uint16_t* const v_pool = static_cast<const uint16_t*>(a.c.v);
   int* const s_pos = reinterpret_cast<int*>(smem + 4 * SM::T_ELEMS) + wave * (kTileRows + 32);
-  uint32_t* const s_bad = reinterpret_cast<uint32_t*>(smem + 4 * SM::T_ELEMS) + SM::POS_BYTES / 4;
+  uint64_t* const s_mask = reinterpret_cast<uint64_t*>(reinterpret_cast<char*>(smem + 4 * SM::T_ELEMS) + SM::POS_BYTES);
+  uint32_t* const s_bad = reinterpret_cast<uint32_t*>(reinterpret_cast<char*>(s_mask) + SM::MASK_BYTES);
   auto stage_k = [&](int st) { return smem + st * SM::T_ELEMS; };
   auto stage_v = [&](int st) { return smem + (2 + st) * SM::T_ELEMS; };
 
@@ -241,10 +288,11 @@ __global__ __launch_bounds__(64 * NW, DH == 256 ? 1 : (NW == 4 ? 2 : 1)) void pa
     // ---- the piece: key tiles [t_begin, t_end) of (b, g, rt)
     int first_tile;
     const int tiles = tiles_of<kTileRows, kRowTile>(sc, P, n, a.inv_g, rt, &first_tile);
-    const int take = !split || tiles - at < x_end - x ? tiles - at : x_end - x;
-    const int t_begin = first_tile + at;
-    const int t_end = t_begin + take;
-    const bool whole = take == tiles;
+    const Piece pc = next_piece(a, w, tiles, at, x);
+    if (pc.from == pc.to) break;   // the share ends with what the row tile costs besides its tiles
+    const int t_begin = first_tile + pc.from;
+    const int t_end = first_tile + pc.to;
+    const bool whole = pc.to - pc.from == tiles;
     const int rows = n * G;
     const int row0 = rt * kRowTile;
     const int wrow0 = row0 + wave * 32;
@@ -259,10 +307,8 @@ __global__ __launch_bounds__(64 * NW, DH == 256 ? 1 : (NW == 4 ? 2 : 1)) void pa
     const bool valid = rho < rows;
     const int token = valid ? div_g(rho, a.inv_g) : tk0;
     const int head = g * G + (valid ? rho - token * G : 0);
-    const int p_own = P + offset_of(sc, b, token);
-    if (h == 0) s_pos[kTileRows + l32] = p_own;   // (read by this wavefront alone)
+    int p_own = P + token;
     float slope2 = 0.f;
-    if constexpr (BIAS) slope2 = sc.slopes[head] * kLog2eF;
     auto token_of = [&](int ln) {
       const int rho_ = wrow0 + (ln & 31);
       return rho_ < rows ? div_g(rho_, a.inv_g) : tk0;
@@ -270,6 +316,7 @@ __global__ __launch_bounds__(64 * NW, DH == 256 ? 1 : (NW == 4 ? 2 : 1)) void pa
 
     // ---- which tiles every row of the workgroup sees whole: those inside [seen_from, seen_to)
     const bool positions = sc.window > 0 || BIAS;
+    const bool mask_here = sc.mask != nullptr && sc.words <= kMaskWords;
     int seen_to = sc.mask != nullptr || (positions && sc.offset != nullptr) ? P : P + tk0 + 1;
     int seen_from = 0;
     if (sc.window > 0) {
@@ -350,6 +397,10 @@ __global__ __launch_bounds__(64 * NW, DH == 256 ? 1 : (NW == 4 ? 2 : 1)) void pa
       __builtin_amdgcn_sched_group_barrier(0x008, 4, 0);
     };
 
+    auto seen_by = [&](int i, int key0) {   // rows of a tile that token i may see, but for the window
+      if (mask_here) return seen_rows(sc, i, P, key0, kend, s_mask + (i - tk0) * sc.words);
+      return seen_rows(sc, b, i, P, key0, kend);
+    };
     // Scores are in base-2 units with MOD, else still to be multiplied by scale * log2(e).
     // Register r of s[kb] is row 32 * kb + 8 * (r / 4) + 4 * h + r % 4 of the tile.
     auto base2_scores = [&](floatx16 (&s)[2]) {
@@ -388,7 +439,7 @@ __global__ __launch_bounds__(64 * NW, DH == 256 ? 1 : (NW == 4 ? 2 : 1)) void pa
       const int key0 = t * kTileRows;
       const int ln = lane_again();
       const int h_ = ln >> 5;
-      const unsigned long long bits = seen_rows(sc, b, token_of(ln), P, key0, kend);
+      const unsigned long long bits = seen_by(token_of(ln), key0);
       int p_i = 0;
       if (positions) {
         p_i = s_pos[kTileRows + (ln & 31)];
@@ -426,7 +477,7 @@ __global__ __launch_bounds__(64 * NW, DH == 256 ? 1 : (NW == 4 ? 2 : 1)) void pa
     // Rows of tile t that this lane's query sees, as bits (again; for the rare tile with values that are not finite).
     auto seen_bits = [&](int t) {
       const int ln = lane_again();
-      unsigned long long bits = seen_rows(sc, b, token_of(ln), P, t * kTileRows, kend);
+      unsigned long long bits = seen_by(token_of(ln), t * kTileRows);
       if (sc.window > 0) {
         const int p_i = s_pos[kTileRows + (ln & 31)];
         for (int k = 0; k < kTileRows; ++k) {
@@ -601,12 +652,27 @@ __global__ __launch_bounds__(64 * NW, DH == 256 ? 1 : (NW == 4 ? 2 : 1)) void pa
     if (whole_from >= whole_to || DH == 256) whole_from = whole_to = t_end;   // none (or no registers for two tiles' scores)
     auto stage_of = [&](int t) { return (t - whole_from) & 1; };
 
-    // ---- prologue: page entries, the first tiles, this lane's query
+    // ---- prologue.  Two round trips to memory: everything that needs no other load (queries, page entries, positions, slopes, mask
+    // words), then the first tiles.
     {
+      u32x4 qv[DSTEPS];
+      const uint16_t* qp = a.q.p + static_cast<int64_t>(b) * a.q.sb + static_cast<int64_t>(token) * a.q.st + static_cast<int64_t>(head) * a.q.sh + 8 * h;
+      if (loader) load_entries(t_begin);
+      uint32_t second = 0;
+      if (loader && t_begin + 1 < t_end) second = page_entry(a.c, b, key_of(t_begin + 1, lane_again()));
+#pragma unroll
+      for (int ds = 0; ds < DSTEPS; ++ds) {
+        qv[ds] = u32x4{0, 0, 0, 0};
+        if (valid) qv[ds] = *reinterpret_cast<const u32x4*>(qp + 16 * ds);
+      }
+      int off = token;
+      if (sc.offset != nullptr) off = sc.offset[static_cast<size_t>(b) * sc.N + token];
+      if constexpr (BIAS) slope2 = sc.slopes[head] * kLog2eF;
+      if (mask_here) {
+        for (int i = tid; i < (tk1 - tk0 + 1) * sc.words; i += kWgThreads)
+          s_mask[i] = sc.mask[(static_cast<size_t>(b) * sc.N + tk0) * sc.words + i];
+      }
       if (loader) {
-        load_entries(t_begin);
-        uint32_t second = 0;
-        if (t_begin + 1 < t_end) second = page_entry(a.c, b, key_of(t_begin + 1, lane_again()));
         asm volatile("" : "+v"(entry), "+v"(second));
         rows_of(t_begin, v_row);
         load_tile(k_pool, stage_k(stage_of(t_begin)), v_row, true);
@@ -616,15 +682,10 @@ __global__ __launch_bounds__(64 * NW, DH == 256 ? 1 : (NW == 4 ? 2 : 1)) void pa
           rows_of(t_begin + 1, v_row);
           load_tile(k_pool, stage_k(stage_of(t_begin + 1)), v_row, true);
         }
+        if (t_begin + 2 < t_end) load_entries(t_begin + 2);
       }
-      const uint16_t* qp = a.q.p + static_cast<int64_t>(b) * a.q.sb + static_cast<int64_t>(token) * a.q.st + static_cast<int64_t>(head) * a.q.sh + 8 * h;
-      u32x4 qv[DSTEPS];
-#pragma unroll
-      for (int ds = 0; ds < DSTEPS; ++ds) {
-        qv[ds] = u32x4{0, 0, 0, 0};
-        if (valid) qv[ds] = *reinterpret_cast<const u32x4*>(qp + 16 * ds);
-      }
-      if (loader && t_begin + 2 < t_end) load_entries(t_begin + 2);
+      p_own = P + (off < 0 ? 0 : (off < kMostOffset ? off : kMostOffset));
+      if (h == 0) s_pos[kTileRows + l32] = p_own;   // (read by this wavefront alone)
       // the compiler's waits for these loads stand here, not inside the loop
 #pragma unroll
       for (int ds = 0; ds < DSTEPS; ds += 4) asm volatile("" : "+v"(qv[ds]), "+v"(qv[ds + 1]), "+v"(qv[ds + 2]), "+v"(qv[ds + 3]));
@@ -705,14 +766,13 @@ __global__ __launch_bounds__(64 * NW, DH == 256 ? 1 : (NW == 4 ? 2 : 1)) void pa
       }
     }
     // the row tile goes on behind this share, and begins in it: the merge at this share's end joins it
-    if (at + take < tiles && at == 0 && tid == 0) {
-      const int last_share = (x + tiles - 1) / w.tiles;
+    if (pc.from == 0 && pc.to < tiles && tid == 0) {
       const int count = rows - row0 < kRowTile ? rows - row0 : kRowTile;
-      a.cut[share] = make_int4(b * a.Hkv + g, row0, count, last_share | (first_piece ? 0 : 1 << 30));
+      a.cut[share] = make_int4(b * a.Hkv + g, row0, count, pc.last | (first_piece ? 0 : 1 << 30));
     }
 
     // ---- on to the next row tile
-    x += split ? take : 1;
+    x += pc.units;
     at = 0;
     first_piece = false;
     if (x < x_end) {

@@ -41,14 +41,15 @@ __device__ __forceinline__ T* chunk_at(T* base, uint32_t chunk) { return base + 
 
 // Which of the 64 rows from `row0` on the new token `i` of a sequence may see, by its mask words or causally (not yet by a
 // window), as bits; rows from `end` on are never seen.
-__device__ __forceinline__ unsigned long long seen_rows(const ScoreArgs& s, int b, int i, int P, int row0, int end) {
+// `w`: the token's mask words.
+template <class W>
+__device__ __forceinline__ unsigned long long seen_rows(const ScoreArgs& s, int i, int P, int row0, int end, const W* w) {
   unsigned long long bits;
   const int d = row0 - P;   // new token that row0 is
   if (s.mask == nullptr) {
     const int count = P + i + 1 - row0;
     bits = count >= 64 ? ~0ull : (count <= 0 ? 0ull : (1ull << count) - 1ull);
   } else {
-    const uint64_t* w = s.mask + (static_cast<size_t>(b) * s.N + i) * s.words;
     if (d >= 0) {
       const int at = d >> 6, shift = d & 63;
       bits = at < s.words ? w[at] >> shift : 0ull;
@@ -64,11 +65,16 @@ __device__ __forceinline__ unsigned long long seen_rows(const ScoreArgs& s, int 
   return bits;
 }
 
-// Position of new token i relative to the prefix.
+__device__ __forceinline__ unsigned long long seen_rows(const ScoreArgs& s, int b, int i, int P, int row0, int end) {
+  return seen_rows(s, i, P, row0, end, s.mask != nullptr ? s.mask + (static_cast<size_t>(b) * s.N + i) * s.words : nullptr);
+}
+
+// Position of new token i relative to the prefix.  (Bounded, so that positions stay 32-bit numbers.)
+constexpr int kMostOffset = (1 << 30) - 1;
 __device__ __forceinline__ int offset_of(const ScoreArgs& s, int b, int i) {
   if (s.offset == nullptr) return i;
   const int o = s.offset[static_cast<size_t>(b) * s.N + i];
-  return o < 0 ? 0 : o;
+  return o < 0 ? 0 : (o < kMostOffset ? o : kMostOffset);
 }
 
 }  // namespace talon

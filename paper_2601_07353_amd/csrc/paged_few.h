@@ -53,7 +53,6 @@ __global__ __launch_bounds__(64 * FewSmem<DH>::NW, DH == 64 ? 4 : (DH == 128 ? 2
   const int h = lane >> 5;
   const ScoreArgs& sc = a.sc;
   const int G = a.G;
-  const bool split = a.cut != nullptr;
   Share w;
   if (!find_share<kFewTile, 32>(a, lane, &w)) return;
   int b = w.b, g = w.g, at = w.at, x = w.x, P = w.P, n = w.n;
@@ -71,12 +70,14 @@ __global__ __launch_bounds__(64 * FewSmem<DH>::NW, DH == 64 ? 4 : (DH == 128 ? 2
   while (x < w.x_end) {
     int first_tile;
     const int tiles = tiles_of<kFewTile, 32>(sc, P, n, a.inv_g, 0, &first_tile);
-    const int take = !split || tiles - at < w.x_end - x ? tiles - at : w.x_end - x;
+    const Piece pc = next_piece(a, w, tiles, at, x);
+    if (pc.from == pc.to) break;   // the share ends with what the row tile costs besides its tiles
+    const int take = pc.to - pc.from;
     const int rows = n * G;
     const int kend = P + n;
     // this wavefront's tiles
-    const int t_begin = first_tile + at + take * wave / NW;
-    const int t_end = first_tile + at + take * (wave + 1) / NW;
+    const int t_begin = first_tile + pc.from + take * wave / NW;
+    const int t_end = first_tile + pc.from + take * (wave + 1) / NW;
 
     // ---- page entries of its first rows (a lane each, 64 pages), this lane's query
     uint32_t pages = 0;
@@ -367,11 +368,10 @@ __global__ __launch_bounds__(64 * FewSmem<DH>::NW, DH == 64 ? 4 : (DH == 128 ? 2
         }
       }
     }
-    if (at + take < tiles && at == 0 && tid == 0)
-      a.cut[w.share] = make_int4(b * a.Hkv + g, 0, rows, ((x + tiles - 1) / w.tiles) | (first_piece ? 0 : 1 << 30));
+    if (pc.from == 0 && pc.to < tiles && tid == 0) a.cut[w.share] = make_int4(b * a.Hkv + g, 0, rows, pc.last | (first_piece ? 0 : 1 << 30));
 
     // ---- on to the next KV head or sequence
-    x += split ? take : 1;
+    x += pc.units;
     at = 0;
     first_piece = false;
     if (x < w.x_end) {

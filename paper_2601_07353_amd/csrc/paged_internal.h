@@ -49,6 +49,7 @@ struct PagedAttnArgs {
   uint32_t inv_g;            // ceil(2^32 / G)
   int slots;                 // most workgroups that take a share of the key tiles
   int least;                 // fewest key tiles of a share
+  int extra;                 // what a row tile costs besides its key tiles, in tiles
   int rows_slot;             // rows of a partial result
   float* part_o;             // [2 * slots][Dh / 8][rows_slot][8]
   float* part_m;             // [2 * slots][rows_slot]

@@ -11,6 +11,7 @@ struct PagedPlan {
   int split;        // 1: row tiles are cut into shares; 0: a workgroup per row tile, nothing to join
   int slots;        // workgroups
   int least;        // fewest key tiles of a share
+  int extra;        // what a row tile costs besides its key tiles, in tiles
   int rows_slot;    // rows of a partial result
   long long tiles;  // key tiles of the call if every sequence is as long as it may be
   size_t off_m, off_l, off_cut, bytes;   // workspace: outputs, maxima, denominators, cuts
@@ -20,8 +21,11 @@ constexpr int kPagedTile = 64;
 constexpr int kPagedWholeTiles = 4;   // up to so many key tiles a row tile is not cut
 constexpr int kPagedLeast = 2;        // fewest key tiles of a share
 constexpr int kPagedFewTile = 32;     // the same for few rows
-constexpr int kPagedFewWhole = 32;
+constexpr int kPagedFewWhole = 24;
 constexpr int kPagedFewLeast = 8;
+constexpr int kPagedPieces = 24;
+constexpr int kPagedExtra = 5;
+constexpr int kPagedFewExtra = 8;
 
 inline PagedPlan paged_plan(int B, int N, int Hq, int Hkv, int Dh, int max_prefix_len) {
   PagedPlan p = {};
@@ -32,7 +36,8 @@ inline PagedPlan paged_plan(int B, int N, int Hq, int Hkv, int Dh, int max_prefi
   const int tile = few ? kPagedFewTile : kPagedTile;
   const long long items = static_cast<long long>(B) * Hkv * ((rows + row_tile - 1) / row_tile);
   const long long most = (static_cast<long long>(max_prefix_len) + N + tile - 1) / tile;
-  p.tiles = items * most;
+  p.extra = few ? kPagedFewExtra : kPagedExtra;
+  p.tiles = items * (most + p.extra);
   p.rows_slot = static_cast<int>(rows < row_tile ? rows : row_tile);
   p.split = most > (few ? kPagedFewWhole : kPagedWholeTiles) ? 1 : 0;
   if (!p.split) {
@@ -41,9 +46,15 @@ inline PagedPlan paged_plan(int B, int N, int Hq, int Hkv, int Dh, int max_prefi
     p.bytes = 256;   // nothing is staged, keep a token size
     return p;
   }
-  p.least = few ? kPagedFewLeast : kPagedLeast;
   const long long slots = few ? (Dh == 64 ? 512 : 256) : (p.waves == 8 || Dh == 256 ? 256 : 512);   // workgroups that the device holds at once
-  const long long enough = (p.tiles + p.least - 1) / p.least;
+  // Few row tiles: as many pieces of each as there are workgroups for, up to what the join reads in three rounds.
+  p.least = few ? kPagedFewLeast : kPagedLeast;
+  if (items * 8 <= slots) {
+    const long long pieces = slots / items < kPagedPieces ? slots / items : kPagedPieces;
+    const long long even = (most + pieces - 1) / pieces;
+    p.least = static_cast<int>(even > p.least ? even : p.least);
+  }
+  const long long enough = (p.tiles + p.least - 1) / p.least + items;   // (also as even pieces of the row tiles)
   p.slots = static_cast<int>(enough < slots ? enough : slots);
   const size_t slot_rows = 2 * static_cast<size_t>(p.slots) * p.rows_slot;
   auto up = [](size_t x) { return (x + 255) / 256 * 256; };
