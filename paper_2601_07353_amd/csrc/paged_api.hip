@@ -166,6 +166,7 @@ int talon_paged_attention(const talon_paged_cache* cache, const talon_view* q, i
   a.lse = out_lse;
   a.B = B; a.Hkv = Hkv; a.G = Hq / Hkv; a.inv_g = inverse_of(a.G);
   a.slots = p.slots; a.least = p.least; a.extra = p.extra; a.rows_slot = p.rows_slot;
+  a.split = p.split;
   if (p.split) {
     if (!workspace || !aligned16(workspace)) { set_error("workspace is NULL or not 16-byte aligned"); return TALON_ERR_INVALID_ARG; }
     if (workspace_bytes < p.bytes) { set_error("workspace of %zu bytes is smaller than the %zu needed", workspace_bytes, p.bytes); return TALON_ERR_WORKSPACE; }
@@ -187,7 +188,8 @@ int talon_paged_attention(const talon_paged_cache* cache, const talon_view* q, i
 int talon_paged_weights(const talon_paged_cache* cache, const talon_view* q, int32_t N, int32_t Hq, const int32_t* n_new,
                         const int32_t* prefix_len, int32_t max_prefix_len, const talon_scores* scores, const float* lse,
                         float decay, const float* prior, float* weights, int64_t stride_b, int64_t stride_h, void* stream) {
-  PagedWeightArgs a = {};
+  PagedWeightArgs wa = {};
+  PagedAttnArgs& a = wa.a;
   int rc = check_cache(cache, "cache", &a.c);
   if (rc) return rc;
   const int B = cache->B, Hkv = cache->Hkv, Dh = cache->Dh;
@@ -203,9 +205,18 @@ int talon_paged_weights(const talon_paged_cache* cache, const talon_view* q, int
     set_error("weights: strides %lld, %lld do not hold %lld rows", (long long)stride_b, (long long)stride_h, most);
     return TALON_ERR_INVALID_ARG;
   }
-  a.lse = lse; a.prior = prior; a.out = weights; a.stride_b = stride_b; a.stride_h = stride_h; a.decay = decay;
+  const long long far = (N > 1 ? a.q.st / 8 * (N - 1) : 0) + a.q.sh / 8 * (Hq / Hkv - 1);
+  if (far >= 1ll << 32) { set_error("q: a sequence's tokens lie more than 64 GiB apart"); return TALON_ERR_UNSUPPORTED; }
+  a.lse = const_cast<float*>(lse);
   a.B = B; a.Hkv = Hkv; a.G = Hq / Hkv; a.inv_g = inverse_of(a.G);
-  return check_hip(launch_paged_weights(a, Dh, cache->dtype, static_cast<hipStream_t>(stream)), "paged weights launch");
+  wa.prior = prior; wa.out = weights; wa.stride_b = stride_b; wa.stride_h = stride_h; wa.decay = decay;
+  const bool few = static_cast<long long>(N) * a.G <= 32;
+  const WeighPlan p = weigh_plan(B, Hkv, Dh, static_cast<int>(most));
+  if (p.tiles >= 1ll << 30) { set_error("%lld key tiles are more than one call takes", p.tiles); return TALON_ERR_UNSUPPORTED; }
+  a.split = 1; a.slots = p.slots; a.least = p.least; a.extra = p.extra;
+  const hipStream_t s = static_cast<hipStream_t>(stream);
+  return check_hip(cache->dtype == TALON_DTYPE_F16 ? launch_paged_weights_f16(wa, Dh, few, s) : launch_paged_weights_bf16(wa, Dh, few, s),
+                   "paged weights launch");
 }
 
 int talon_paged_evict(const talon_paged_cache* cache, const talon_paged_cache* dst, const int32_t* len, int32_t max_len,

@@ -90,8 +90,13 @@ struct PagedSmem {
 };
 
 // Key tiles [*first, *first + result) of row tile rt of a sequence.
-template <int TILE, int ROW_TILE>
+// ALL: of all rows, whatever sees them.
+template <int TILE, int ROW_TILE, bool ALL = false>
 __device__ __forceinline__ int tiles_of(const ScoreArgs& sc, int P, int n, uint32_t inv_g, int rt, int* first) {
+  if constexpr (ALL) {
+    *first = 0;
+    return (P + n + TILE - 1) / TILE;
+  }
   int last = div_g((rt + 1) * ROW_TILE - 1, inv_g);
   last = last < n - 1 ? last : n - 1;
   const int end = sc.mask != nullptr ? P + n : P + last + 1;
@@ -116,10 +121,10 @@ struct Share {
 
 // Every wavefront works this out from the lengths, lane l for sequences l, l + 64, ...  (Loops, not unrolled copies: a workgroup
 // comes here with a cold instruction cache.)  False: nothing to do.
-template <int TILE, int ROW_TILE>
+template <int TILE, int ROW_TILE, bool ALL = false>
 __device__ __forceinline__ bool find_share(const PagedAttnArgs& a, int lane, Share* w) {
   const ScoreArgs& sc = a.sc;
-  const bool split = a.cut != nullptr;
+  const bool split = a.split != 0;
   // Workgroup ids are dealt round-robin to the 8 XCDs: neighbouring shares, which read the same rows of K and V where a sequence
   // has several row tiles, go to one XCD and its L2.  (The grid is a multiple of 8.)
   const int share = static_cast<int>(blockIdx.x & 7u) * (static_cast<int>(gridDim.x) >> 3) + static_cast<int>(blockIdx.x >> 3);
@@ -129,13 +134,13 @@ __device__ __forceinline__ bool find_share(const PagedAttnArgs& a, int lane, Sha
     sum = pieces = P = n = 0;
     if (bb < a.B) {
       clamped_lengths(a.c, sc.prefix_len[bb], sc.n_new[bb], sc.max_prefix_len, sc.N, &P, &n);
-      const int row_tiles = (n * a.G + ROW_TILE - 1) / ROW_TILE;
+      const int row_tiles = ALL ? (P + n > 0 ? 1 : 0) : (n * a.G + ROW_TILE - 1) / ROW_TILE;
       if (!split) sum = row_tiles;
       else {
         int first;
 #pragma unroll 1
         for (int r = 0; r < row_tiles; ++r) {
-          const int tiles = tiles_of<TILE, ROW_TILE>(sc, P, n, a.inv_g, r, &first);
+          const int tiles = tiles_of<TILE, ROW_TILE, ALL>(sc, P, n, a.inv_g, r, &first);
           sum += tiles + a.extra;
           pieces += pieces_of(tiles);
         }
@@ -162,7 +167,7 @@ __device__ __forceinline__ bool find_share(const PagedAttnArgs& a, int lane, Sha
   }
   tiles = alone ? 1 : (tiles < a.least ? a.least : tiles);
   const long long x0 = static_cast<long long>(share) * tiles;
-  if (split && threadIdx.x == 0 && share < a.slots) a.cut[share] = make_int4(0, 0, 0, 0);
+  if (a.cut != nullptr && threadIdx.x == 0 && share < a.slots) a.cut[share] = make_int4(0, 0, 0, 0);
   if (x0 >= total) return false;
   const int x = static_cast<int>(x0);
   int before = 0, b = 0, at = 0, mine = 0;
@@ -194,7 +199,7 @@ __device__ __forceinline__ bool find_share(const PagedAttnArgs& a, int lane, Sha
   if (split) {
 #pragma unroll 1
     for (int first;; ++rt) {
-      const int t = tiles_of<TILE, ROW_TILE>(sc, P, n, a.inv_g, rt, &first);
+      const int t = tiles_of<TILE, ROW_TILE, ALL>(sc, P, n, a.inv_g, rt, &first);
       const int k = alone ? pieces_of(t) : t + a.extra;
       if (at < k) {
         if (alone) {   // piece `at` of k even ones
@@ -223,7 +228,7 @@ struct Piece {
   int last;        // share of the row tile's last tile
 };
 __device__ __forceinline__ Piece next_piece(const PagedAttnArgs& a, const Share& w, int tiles, int at, int x) {
-  if (a.cut == nullptr) return {0, tiles, 1, 0};
+  if (!a.split) return {0, tiles, 1, 0};
   if (w.take > 0) return {at, at + w.take, w.x_end - x, w.last};
   const int rest = tiles + a.extra - at;
   const int units = rest < w.x_end - x ? rest : w.x_end - x;
@@ -253,7 +258,6 @@ __global__ __launch_bounds__(64 * NW, DH == 256 ? 1 : (NW == 4 ? 2 : 1)) void pa
   const ScoreArgs& sc = a.sc;
   const int G = a.G;
 
-  const bool split = a.cut != nullptr;   // else a share is a row tile
   Share w;
   if (!find_share<kTileRows, kRowTile>(a, lane, &w)) return;
   int b = w.b, g = w.g, rt = w.rt, at = w.at, x = w.x, P = w.P, n = w.n;

@@ -44,9 +44,10 @@ struct PagedAttnArgs {
   PagedRows c;
   ScoreArgs sc;
   RowsView q, out;
-  float* lse;                // [B][N][Hq] or NULL
+  float* lse;                // [B][N][Hq] or NULL (written by attention, read by the weights)
   int B, Hkv, G;
   uint32_t inv_g;            // ceil(2^32 / G)
+  int split;                 // 1: shares of the line of key tiles; 0: a row tile per workgroup
   int slots;                 // most workgroups that take a share of the key tiles
   int least;                 // fewest key tiles of a share
   int extra;                 // what a row tile costs besides its key tiles, in tiles
@@ -54,20 +55,15 @@ struct PagedAttnArgs {
   float* part_o;             // [2 * slots][Dh / 8][rows_slot][8]
   float* part_m;             // [2 * slots][rows_slot]
   float* part_l;
-  int4* cut;                 // [slots] the row tile that a share's end cuts, see paged_attention.h; NULL: none can be cut
+  int4* cut;                 // [slots] the row tile that a share's end cuts, see paged_attention.h; NULL: nothing is joined
 };
 
 struct PagedWeightArgs {
-  PagedRows c;
-  ScoreArgs sc;
-  RowsView q;
-  const float* lse;
+  PagedAttnArgs a;           // cache, scores, queries, lse (read), shares
   const float* prior;        // or NULL
   float* out;
   int64_t stride_b, stride_h;
   float decay;
-  int B, Hkv, G;
-  uint32_t inv_g;
 };
 
 struct RotaryArgs {
@@ -112,7 +108,8 @@ hipError_t launch_paged_attention_bf16_256(const PagedAttnArgs& a, int waves, hi
 hipError_t launch_paged_attention_f16_64(const PagedAttnArgs& a, int waves, hipStream_t s);
 hipError_t launch_paged_attention_f16_128(const PagedAttnArgs& a, int waves, hipStream_t s);
 hipError_t launch_paged_attention_f16_256(const PagedAttnArgs& a, int waves, hipStream_t s);
-hipError_t launch_paged_weights(const PagedWeightArgs& a, int Dh, int dtype, hipStream_t s);
+hipError_t launch_paged_weights_bf16(const PagedWeightArgs& wa, int Dh, bool few, hipStream_t s);
+hipError_t launch_paged_weights_f16(const PagedWeightArgs& wa, int Dh, bool few, hipStream_t s);
 hipError_t launch_rotary_store(const RotaryArgs& a, int dtype, hipStream_t s);
 hipError_t launch_paged_evict(const EvictArgs& a, hipStream_t s);
 hipError_t launch_paged_compact(const CompactArgs& a, hipStream_t s);

@@ -26,6 +26,7 @@ constexpr int kPagedFewLeast = 8;
 constexpr int kPagedPieces = 24;
 constexpr int kPagedExtra = 5;
 constexpr int kPagedFewExtra = 8;
+constexpr int kWeighExtra = 4;
 
 inline PagedPlan paged_plan(int B, int N, int Hq, int Hkv, int Dh, int max_prefix_len) {
   PagedPlan p = {};
@@ -62,6 +63,22 @@ inline PagedPlan paged_plan(int B, int N, int Hq, int Hkv, int Dh, int max_prefi
   p.off_l = p.off_m + up(slot_rows * sizeof(float));
   p.off_cut = p.off_l + up(slot_rows * sizeof(float));
   p.bytes = p.off_cut + up(static_cast<size_t>(p.slots) * 16);
+  return p;
+}
+
+// Attention weights of few queries: the same shares, of all rows of the sequences.
+struct WeighPlan {
+  int slots, least, extra;
+  long long tiles;
+};
+inline WeighPlan weigh_plan(int B, int Hkv, int Dh, int rows) {
+  WeighPlan p = {};
+  const long long items = static_cast<long long>(B) * Hkv, most = (static_cast<long long>(rows) + kPagedFewTile - 1) / kPagedFewTile;
+  p.least = kPagedFewLeast;
+  p.extra = kWeighExtra;
+  p.tiles = items * (most + p.extra);
+  const long long slots = Dh == 64 ? 512 : 256, enough = (p.tiles + p.least - 1) / p.least + items;
+  p.slots = static_cast<int>(enough < slots ? enough : slots);
   return p;
 }
 

@@ -1,0 +1,8 @@
+// The kernels of paged_weights.h for a cache in f16.
+#include "paged_weights.h"
+
+namespace talon {
+
+hipError_t launch_paged_weights_f16(const PagedWeightArgs& wa, int Dh, bool few, hipStream_t s) { return launch_weights<true>(wa, Dh, few, s); }
+
+}  // namespace talon
