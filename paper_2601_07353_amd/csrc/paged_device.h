@@ -11,7 +11,10 @@ constexpr float kLog2eF = 1.4426950408889634f;
 constexpr float kLn2F = 0.6931471805599453f;
 
 // x / G for 0 <= x < 2^24, G <= 128: exact, since x * (inv_g * G - 2^32) < 2^32.
-__device__ __forceinline__ int div_g(int x, uint32_t inv_g) { return inv_g == 0u ? x : static_cast<int>(__umulhi(static_cast<uint32_t>(x), inv_g)); }
+// (inv_g is 0 for G = 1; without a branch, which would end a block.)
+__device__ __forceinline__ int div_g(int x, uint32_t inv_g) {
+  return static_cast<int>(__umulhi(static_cast<uint32_t>(x), inv_g)) + (x & -static_cast<int>(inv_g == 0u));
+}
 
 // Rows that a sequence has in the cache and rows that are new, whatever the device's numbers say: neither
 // points beyond what the call or the page table allows for.

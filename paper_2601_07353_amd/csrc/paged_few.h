@@ -89,24 +89,29 @@ __global__ __launch_bounds__(64 * FewSmem<DH>::NW, DH == 64 ? 4 : (DH == 128 ? 2
       int i = at64 * 64 + lane;
       i = i < a.c.max_pages ? i : a.c.max_pages - 1;
       pages = static_cast<uint32_t>(a.c.table[static_cast<size_t>(b) * a.c.max_pages + i]);
-      asm volatile("" : "+v"(pages));   // waited for here
     };
     const bool valid = l32 < rows;
     const int token = valid ? div_g(l32, a.inv_g) : 0;
     const int head = g * G + (valid ? l32 - token * G : 0);
     x8 bq[DSTEPS];
-    {
-      const uint16_t* qp = a.q.p + static_cast<int64_t>(b) * a.q.sb + static_cast<int64_t>(token) * a.q.st + static_cast<int64_t>(head) * a.q.sh + 8 * h;
-#pragma unroll
-      for (int ds = 0; ds < DSTEPS; ++ds) {
-        u32x4 v = u32x4{0, 0, 0, 0};
-        if (valid) v = *reinterpret_cast<const u32x4*>(qp + 16 * ds);
-        bq[ds] = __builtin_bit_cast(x8, v);
-      }
-    }
     const int p_own = P + offset_of(sc, b, token);
     float slope2 = 0.f;
     if constexpr (BIAS) slope2 = sc.slopes[head] * kLog2eF;
+    {
+      const uint16_t* qp = a.q.p + static_cast<int64_t>(b) * a.q.sb + static_cast<int64_t>(token) * a.q.st + static_cast<int64_t>(head) * a.q.sh + 8 * h;
+      u32x4 qv[DSTEPS];
+#pragma unroll
+      for (int ds = 0; ds < DSTEPS; ++ds) {
+        qv[ds] = u32x4{0, 0, 0, 0};
+        if (valid) qv[ds] = *reinterpret_cast<const u32x4*>(qp + 16 * ds);
+      }
+      load_pages(first_tile + pc.from + take * wave / NW);
+      // (the compiler's wait for these loads stands here: inside the loop it would count the tile loads too)
+#pragma unroll
+      for (int ds = 0; ds < DSTEPS; ds += 4) asm volatile("" : "+v"(qv[ds]), "+v"(qv[ds + 1]), "+v"(qv[ds + 2]), "+v"(qv[ds + 3]));
+#pragma unroll
+      for (int ds = 0; ds < DSTEPS; ++ds) bq[ds] = __builtin_bit_cast(x8, qv[ds]);
+    }
     const bool positions = sc.window > 0 || BIAS;
     int seen_to = sc.mask != nullptr || (positions && sc.offset != nullptr) ? P : P + 1;   // rows that every query sees: [seen_from, seen_to)
     int seen_from = 0;
@@ -119,6 +124,7 @@ __global__ __launch_bounds__(64 * FewSmem<DH>::NW, DH == 64 ? 4 : (DH == 128 ? 2
     uint32_t row_at[LOADS];
     auto rows_of = [&](int t) {
       load_pages(t);
+      asm volatile("" : "+v"(pages));   // (waited for here where it was read anew)
       int key = t * kFewTile + l32;
       key = key < kend ? key : kend - 1;
       const uint32_t entry = static_cast<uint32_t>(__builtin_amdgcn_ds_bpermute(((key >> a.c.page_shift) & 63) * 4, static_cast<int>(pages)));

@@ -40,12 +40,14 @@ __device__ __forceinline__ bool sees_row(const ScoreArgs& s, int b, int i, int P
 
 constexpr int kNobody = -1;   // token of a row behind the last query
 
+constexpr int kQueryTile = 128;
+
 // A query's entry in the tables of a tile: lse (base 2), token, position, slope (base 2).
 struct QueryTables {
-  float lse[64];
-  int token[64];
-  int pos[64];
-  float slope[64];
+  float lse[kQueryTile];
+  int token[kQueryTile];
+  int pos[kQueryTile];
+  float slope[kQueryTile];
 };
 
 // Sum over the 16 queries of this half in a 32 x 32 block of products: register r is query 8 * (r / 4) + 4 * h + r % 4.  `whole`: each
@@ -54,47 +56,51 @@ template <bool CAP, bool BIAS>
 __device__ __forceinline__ float block_sum(const PagedAttnArgs& a, floatx16 s, const QueryTables& t, int q0, int h, bool whole, int b, int P, int key, int pos,
                                            bool real, int count) {
   const ScoreArgs& sc = a.sc;
-  float sum = 0.f;
   if constexpr (CAP) {
 #pragma unroll
     for (int r = 0; r < 16; ++r) s[r] = sc.cap_log2e * tanh_of(s[r] * sc.cap_in);
   }
-  const int window = sc.window > 0 ? sc.window : 0x7FFFFFFF;
+  float x[16];
 #pragma unroll
   for (int q4 = 0; q4 < 4; ++q4) {
-    if (8 * q4 >= count) break;   // uniform
     const int at = q0 + 8 * q4 + 4 * h;
     const float4 l4 = *reinterpret_cast<const float4*>(&t.lse[at]);
     const float ls[4] = {l4.x, l4.y, l4.z, l4.w};
-    float x[4];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) x[e] = CAP ? s[4 * q4 + e] - ls[e] : __builtin_fmaf(s[4 * q4 + e], sc.scale_log2e, -ls[e]);
+    for (int e = 0; e < 4; ++e) x[4 * q4 + e] = CAP ? s[4 * q4 + e] - ls[e] : __builtin_fmaf(s[4 * q4 + e], sc.scale_log2e, -ls[e]);
     if constexpr (BIAS) {
       const int4 p4 = *reinterpret_cast<const int4*>(&t.pos[at]);
       const float4 f4 = *reinterpret_cast<const float4*>(&t.slope[at]);
       const int ps[4] = {p4.x, p4.y, p4.z, p4.w};
       const float fs[4] = {f4.x, f4.y, f4.z, f4.w};
 #pragma unroll
-      for (int e = 0; e < 4; ++e) x[e] = __builtin_fmaf(-fs[e], fabsf(static_cast<float>(ps[e] - pos)), x[e]);
+      for (int e = 0; e < 4; ++e) x[4 * q4 + e] = __builtin_fmaf(-fs[e], fabsf(static_cast<float>(ps[e] - pos)), x[4 * q4 + e]);
     }
-    if (whole && count >= 8 * q4 + 8) {
+  }
+  float sum[4] = {0.f, 0.f, 0.f, 0.f};
+  if (whole && count == 32) {   // uniform; nothing else in the way of the exponentials
 #pragma unroll
-      for (int e = 0; e < 4; ++e) sum += __builtin_amdgcn_exp2f(x[e]);
-    } else if (whole) {
+    for (int r = 0; r < 16; ++r) sum[r % 4] += __builtin_amdgcn_exp2f(x[r]);
+  } else if (whole) {
 #pragma unroll
-      for (int e = 0; e < 4; ++e) sum += 8 * q4 + 4 * h + e < count ? __builtin_amdgcn_exp2f(x[e]) : 0.f;
-    } else {
+    for (int r = 0; r < 16; ++r)
+      if (8 * (r / 4) < count) sum[r % 4] += 8 * (r / 4) + 4 * h + r % 4 < count ? __builtin_amdgcn_exp2f(x[r]) : 0.f;
+  } else {
+    const int window = sc.window > 0 ? sc.window : 0x7FFFFFFF;
+#pragma unroll
+    for (int q4 = 0; q4 < 4; ++q4) {
+      const int at = q0 + 8 * q4 + 4 * h;
       const int4 t4 = *reinterpret_cast<const int4*>(&t.token[at]);
       const int4 p4 = *reinterpret_cast<const int4*>(&t.pos[at]);
       const int ts[4] = {t4.x, t4.y, t4.z, t4.w}, ps[4] = {p4.x, p4.y, p4.z, p4.w};
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         const bool seen = real && ts[e] != kNobody && ps[e] - pos < window && sees_row(sc, b, ts[e], P, key);
-        sum += seen ? __builtin_amdgcn_exp2f(x[e]) : 0.f;
+        sum[e] += seen ? __builtin_amdgcn_exp2f(x[4 * q4 + e]) : 0.f;
       }
     }
   }
-  return sum;
+  return (sum[0] + sum[1]) + (sum[2] + sum[3]);
 }
 
 __device__ __forceinline__ float both_halves(float v) {
@@ -102,35 +108,48 @@ __device__ __forceinline__ float both_halves(float v) {
   return __int_as_float(static_cast<int>(sw[0])) + __int_as_float(static_cast<int>(sw[1]));
 }
 
-// ---- many queries: a workgroup of four wavefronts owns 128 rows of the cache, 32 a wavefront, whose keys stay in registers, and
-// streams the queries that may see them through LDS, 64 (token, head) rows a tile (32 of heads of 256), two stages.  Bound: the
-// exponentials (a quarter of the vector rate) and the matrix product.
+// ---- many queries: a workgroup of eight wavefronts owns 64 rows of the cache and streams the queries that may see them through LDS,
+// 128 (token, head) rows a tile, two stages.  A wavefront has 32 of the rows, whose keys stay in its registers, and 32 queries of
+// every tile; the four that share rows add theirs in LDS at the end.  Bound: the exponentials (a quarter of the vector rate) and
+// the matrix product, which hardly run at the same time.  The time of a workgroup is short against the call's, so that the last
+// ones cost little: 512 tokens at 8192 rows 71 us, against 77 with four wavefronts and tiles of 64 rows and 82 with four wavefronts
+// on 128 rows.
+constexpr int kWeighRows = 64;
+
+template <int DH>
+struct WeighSmem {
+  static constexpr int STAGE = kQueryTile * DH;
+  static constexpr int BYTES = 2 * STAGE * 2 + 2 * static_cast<int>(sizeof(QueryTables)) + 3 * kWeighRows * 4;
+};
+
 template <bool F16, int DH, bool CAP, bool BIAS>
-__global__ __launch_bounds__(256, DH == 256 ? 1 : 3) void paged_weights_kernel(PagedWeightArgs wa) {
+__global__ __launch_bounds__(512, DH == 256 ? 2 : 4) void paged_weights_kernel(PagedWeightArgs wa) {
   using ST = Storage<F16>;
   using x8 = typename ST::x8;
   using SM = PagedSmem<DH>;
   const PagedAttnArgs& a = wa.a;
   constexpr int CPR = DH / 8;
   constexpr int DSTEPS = DH / 16;
-  constexpr int QT = DH == 256 ? 32 : 64;
+  constexpr int QT = kQueryTile;
   constexpr int ROWS_PER_LOAD = 64 / CPR;
-  constexpr int LOADS = QT / 4 / ROWS_PER_LOAD;
-  __shared__ __attribute__((aligned(16))) uint16_t s_q[2][QT * DH];
-  __shared__ __attribute__((aligned(16))) QueryTables s_t[2];
+  constexpr int LOADS = QT / 8 / ROWS_PER_LOAD;
+  extern __shared__ __attribute__((aligned(16))) uint16_t smem[];
+  QueryTables* const s_t = reinterpret_cast<QueryTables*>(smem + 2 * WeighSmem<DH>::STAGE);
+  float* const s_part = reinterpret_cast<float*>(s_t + 2);
   const ScoreArgs& sc = a.sc;
   const int b = blockIdx.z, g = blockIdx.y;
   int P, n;
   clamped_lengths(a.c, sc.prefix_len[b], sc.n_new[b], sc.max_prefix_len, sc.N, &P, &n);
   const int len = P + n;
-  const int key0 = static_cast<int>(blockIdx.x) * 128;
+  const int key0 = static_cast<int>(blockIdx.x) * kWeighRows;
   if (key0 >= len) return;
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
   const int l32 = lane & 31, h = lane >> 5;
   const int G = a.G;
 
   // ---- this lane's key (a row past the end reads the last one; it gets nothing)
-  const int key = key0 + 32 * wave + l32;
+  const int key = key0 + 32 * (wave & 1) + l32;
+  const int q0 = 32 * (wave >> 1);   // its queries of a tile
   const bool real = key < len;
   int pos = key;
   x8 bk[DSTEPS];
@@ -140,12 +159,18 @@ __global__ __launch_bounds__(256, DH == 256 ? 1 : 3) void paged_weights_kernel(P
     if (real && key >= P) pos = P + offset_of(sc, b, key - P);
     if (__ballot(entry >= a.c.num_pages) != 0ull && lane == 0) report(a.c, b, TALON_STATUS_BAD_PAGE);
     const uint16_t* kp = chunk_at(static_cast<const uint16_t*>(a.c.k), row_chunk(a.c, entry, row, g) + h);
+    u32x4 kv[DSTEPS];
 #pragma unroll
-    for (int ds = 0; ds < DSTEPS; ++ds) bk[ds] = __builtin_bit_cast(x8, *reinterpret_cast<const uint4*>(kp + 16 * ds));
+    for (int ds = 0; ds < DSTEPS; ++ds) kv[ds] = *reinterpret_cast<const u32x4*>(kp + 16 * ds);
+    // (the compiler's wait for these loads stands here: inside the loop it would count the queries' loads too)
+#pragma unroll
+    for (int ds = 0; ds < DSTEPS; ds += 4) asm volatile("" : "+v"(kv[ds]), "+v"(kv[ds + 1]), "+v"(kv[ds + 2]), "+v"(kv[ds + 3]));
+#pragma unroll
+    for (int ds = 0; ds < DSTEPS; ++ds) bk[ds] = __builtin_bit_cast(x8, kv[ds]);
   }
 
   // ---- the queries that may see a row of this workgroup: tokens [i_from, i_to)
-  const int last_key = key0 + 128 < len ? key0 + 127 : len - 1;
+  const int last_key = key0 + kWeighRows < len ? key0 + kWeighRows - 1 : len - 1;
   const int i_from = sc.mask == nullptr && key0 > P ? key0 - P : 0;
   int i_to = n;
   if (sc.window > 0 && sc.offset == nullptr) {   // P + i - last_key < window
@@ -161,16 +186,18 @@ __global__ __launch_bounds__(256, DH == 256 ? 1 : 3) void paged_weights_kernel(P
   const uint16_t* const qb = a.q.p + static_cast<int64_t>(b) * a.q.sb + static_cast<int64_t>(g) * G * a.q.sh;
   const uint32_t token_chunks = static_cast<uint32_t>(a.q.st / 8), head_chunks = static_cast<uint32_t>(a.q.sh / 8);
   float lse_next = 0.f, slope_next = 0.f;
-  int token_next = kNobody, pos_next = 0;
+  int token_next = kNobody, off_next = 0;   // (as loaded: used when the next tile has landed)
   auto load_queries = [&](int r0, int st) {
+    // (a lane finds one of this wavefront's 16 rows, the lanes of a load take their rows' places from it: integer products are slow)
+    int rho_l = r0 + wave * 16 + (lane & 15);
+    rho_l = rho_l < rows ? rho_l : rows - 1;
+    const int token_l = div_g(rho_l, a.inv_g);
+    const int place = static_cast<int>(static_cast<uint32_t>(token_l) * token_chunks + static_cast<uint32_t>(rho_l - token_l * G) * head_chunks);
 #pragma unroll
     for (int i = 0; i < LOADS; ++i) {
       const int u = (wave * LOADS + i) * ROWS_PER_LOAD;
-      int rho = r0 + u + lane / CPR;
-      rho = rho < rows ? rho : rows - 1;
-      const int token = div_g(rho, a.inv_g);
-      const uint32_t chunk = static_cast<uint32_t>(token) * token_chunks + static_cast<uint32_t>(rho - token * G) * head_chunks;
-      global_to_lds(chunk_at(qb, chunk + ((lane % CPR) ^ SM::kswz(u + lane / CPR))), &s_q[st][u * DH]);
+      const uint32_t chunk = static_cast<uint32_t>(__builtin_amdgcn_ds_bpermute((i * ROWS_PER_LOAD + lane / CPR) * 4, place));
+      global_to_lds(chunk_at(qb, chunk + ((lane % CPR) ^ SM::kswz(u + lane / CPR))), smem + st * WeighSmem<DH>::STAGE + u * DH);
     }
     if (tid < QT) {
       const int rho = r0 + tid;
@@ -179,18 +206,19 @@ __global__ __launch_bounds__(256, DH == 256 ? 1 : 3) void paged_weights_kernel(P
       if (rho < r_end) {
         token_next = div_g(rho, a.inv_g);
         const int head = g * G + rho - token_next * G;
-        lse_next = a.lse[(static_cast<size_t>(b) * sc.N + token_next) * (a.Hkv * G) + head] * kLog2eF;
-        pos_next = P + offset_of(sc, b, token_next);
-        if constexpr (BIAS) slope_next = sc.slopes[head] * kLog2eF;
+        lse_next = a.lse[(static_cast<size_t>(b) * sc.N + token_next) * (a.Hkv * G) + head];
+        off_next = token_next;
+        if (sc.offset != nullptr) off_next = sc.offset[static_cast<size_t>(b) * sc.N + token_next];
+        if constexpr (BIAS) slope_next = sc.slopes[head];
       }
     }
   };
   auto store_tables = [&](int st) {
     if (tid < QT) {
-      s_t[st].lse[tid] = lse_next;
+      s_t[st].lse[tid] = lse_next * kLog2eF;
       s_t[st].token[tid] = token_next;
-      s_t[st].pos[tid] = pos_next;
-      if constexpr (BIAS) s_t[st].slope[tid] = slope_next;
+      s_t[st].pos[tid] = P + (off_next < 0 ? 0 : (off_next < kMostOffset ? off_next : kMostOffset));
+      if constexpr (BIAS) s_t[st].slope[tid] = slope_next * kLog2eF;
     }
   };
   auto landed = [&]() {
@@ -210,22 +238,17 @@ __global__ __launch_bounds__(256, DH == 256 ? 1 : 3) void paged_weights_kernel(P
     const bool more = r0 + QT < r_end;
     if (more) load_queries(r0 + QT, st ^ 1);
     const bool whole = near && r0 + QT <= r_end && div_g(r0, a.inv_g) >= seen_from;
-    float part = 0.f;
+    floatx16 s;
 #pragma unroll
-    for (int qb_ = 0; qb_ < QT / 32; ++qb_) {
-      floatx16 s;
+    for (int r = 0; r < 16; ++r) s[r] = 0.f;
+    const int row = q0 + l32;
+    const int swz = SM::kswz(row);
 #pragma unroll
-      for (int r = 0; r < 16; ++r) s[r] = 0.f;
-      const int row = 32 * qb_ + l32;
-      const int swz = SM::kswz(row);
-#pragma unroll
-      for (int ds = 0; ds < DSTEPS; ++ds) {
-        const x8 aq = __builtin_bit_cast(x8, *reinterpret_cast<const uint4*>(&s_q[st][row * DH + ((2 * ds + h) ^ swz) * 8]));
-        s = ST::mfma(aq, bk[ds], s);
-      }
-      part += block_sum<CAP, BIAS>(a, s, s_t[st], 32 * qb_, h, whole, b, P, key, pos, real, 32);
+    for (int ds = 0; ds < DSTEPS; ++ds) {
+      const x8 aq = __builtin_bit_cast(x8, *reinterpret_cast<const uint4*>(smem + st * WeighSmem<DH>::STAGE + row * DH + ((2 * ds + h) ^ swz) * 8));
+      s = ST::mfma(aq, bk[ds], s);
     }
-    acc += part;
+    acc += block_sum<CAP, BIAS>(a, s, s_t[st], q0, h, whole, b, P, key, pos, real, 32);
     if ((count & 15) == 0) {
       sum += acc;
       acc = 0.f;
@@ -233,8 +256,12 @@ __global__ __launch_bounds__(256, DH == 256 ? 1 : 3) void paged_weights_kernel(P
     if (more) store_tables(st ^ 1);
     landed();
   }
-  const float total = both_halves(sum + acc);
-  if (h == 0 && real) {
+  float total = both_halves(sum + acc);
+  if (q0 != 0 && h == 0) s_part[32 * (wave - 2) + l32] = total;
+  __syncthreads();
+  if (q0 == 0 && h == 0 && real) {
+#pragma unroll
+    for (int v = 0; v < 3; ++v) total += s_part[32 * (2 * v + wave) + l32];
     const size_t at = static_cast<size_t>(b) * wa.stride_b + static_cast<size_t>(g) * wa.stride_h + key;
     wa.out[at] = total + (wa.prior != nullptr && key < P ? wa.decay * wa.prior[at] : 0.f);
   }
@@ -329,11 +356,11 @@ __global__ __launch_bounds__(64 * WeighFewSmem<DH>::NW, DH == 64 ? 4 : (DH == 12
       const int token = valid ? div_g(l32, a.inv_g) : 0;
       const int head = g * G + (valid ? l32 - token * G : 0);
       const uint16_t* qp = a.q.p + static_cast<int64_t>(b) * a.q.sb + static_cast<int64_t>(token) * a.q.st + static_cast<int64_t>(head) * a.q.sh + 8 * h;
+      u32x4 qv[DSTEPS];
 #pragma unroll
       for (int ds = 0; ds < DSTEPS; ++ds) {
-        u32x4 v = u32x4{0, 0, 0, 0};
-        if (valid) v = *reinterpret_cast<const u32x4*>(qp + 16 * ds);
-        aq[ds] = __builtin_bit_cast(x8, v);
+        qv[ds] = u32x4{0, 0, 0, 0};
+        if (valid) qv[ds] = *reinterpret_cast<const u32x4*>(qp + 16 * ds);
       }
       if (h == 0) {
         s_t.lse[l32] = valid ? a.lse[(static_cast<size_t>(b) * sc.N + token) * (a.Hkv * G) + head] * kLog2eF : __builtin_huge_valf();
@@ -341,6 +368,11 @@ __global__ __launch_bounds__(64 * WeighFewSmem<DH>::NW, DH == 64 ? 4 : (DH == 12
         s_t.pos[l32] = P + offset_of(sc, b, token);
         if constexpr (BIAS) s_t.slope[l32] = valid ? sc.slopes[head] * kLog2eF : 0.f;
       }
+      // (the compiler's wait for these loads stands here: inside the loop it would count the tile loads too)
+#pragma unroll
+      for (int ds = 0; ds < DSTEPS; ds += 4) asm volatile("" : "+v"(qv[ds]), "+v"(qv[ds + 1]), "+v"(qv[ds + 2]), "+v"(qv[ds + 3]));
+#pragma unroll
+      for (int ds = 0; ds < DSTEPS; ++ds) aq[ds] = __builtin_bit_cast(x8, qv[ds]);
       __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
       __builtin_amdgcn_wave_barrier();
     }
@@ -402,7 +434,11 @@ hipError_t launch_weights_one(const PagedWeightArgs& wa, bool few, hipStream_t s
     hipLaunchKernelGGL(kern, dim3((wa.a.slots + 7) / 8 * 8), dim3(64 * WeighFewSmem<DH>::NW), WeighFewSmem<DH>::BYTES, s, wa);
   } else {
     const int most = wa.a.sc.max_prefix_len + wa.a.sc.N < wa.a.c.capacity ? wa.a.sc.max_prefix_len + wa.a.sc.N : wa.a.c.capacity;
-    hipLaunchKernelGGL((paged_weights_kernel<F16, DH, CAP, BIAS>), dim3((most + 127) / 128, wa.a.Hkv, wa.a.B), dim3(256), 0, s, wa);
+    auto kern = paged_weights_kernel<F16, DH, CAP, BIAS>;
+    static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize,
+                                                       WeighSmem<DH>::BYTES);
+    if (attr != hipSuccess) return attr;
+    hipLaunchKernelGGL(kern, dim3((most + kWeighRows - 1) / kWeighRows, wa.a.Hkv, wa.a.B), dim3(512), WeighSmem<DH>::BYTES, s, wa);
   }
   return hipGetLastError();
 }
