@@ -76,6 +76,8 @@ struct RotaryArgs {
   const int32_t* axis;       // [pairs] or NULL
   const float* inv_freq;     // [pairs]
   int B, N, Hq, Hkv, Dh, pairs, axes, interleaved;
+  int units;                 // pieces of a head (set by the launch)
+  uint32_t inv_units;        // ceil(2^32 / units), 0 for 1
 };
 
 struct EvictArgs {

@@ -22,15 +22,20 @@ union Chunk {
 
 // ---- rotary positions and the write into the pages.
 // angle(token, f) = (base + pos[axis(f)][token]) * inv_freq[f];  (x1, x2) -> (x1 cos - x2 sin, x2 cos + x1 sin)
-// A workgroup takes TOKENS tokens.  First the angles' sines and cosines, one (token, f) per thread, to LDS: the product and its
-// reduction to one turn are formed in 64 bits (a position of 10^5 in fp32 has lost 2^-8 of a turn), the rest in fp32.  Then the
-// heads' values, two chunks of 16 bytes per thread: the eight first and the eight second values of eight pairs, so that a
-// value is read and written by one thread and q may be rotated in place.
-template <bool F16, int TOKENS>
+// A workgroup takes a token.  The angles' sines and cosines, one f per thread, go to LDS: the product and its
+// reduction to one turn are formed in 64 bits (a position of 10^5 in fp32 has lost 2^-8 of a turn), the rest in fp32.  The heads'
+// values are two chunks of 16 bytes per thread: the eight first and the eight second values of eight pairs, so that a
+// value is read and written by one thread and q may be rotated in place; values that are copied go the same way.  A thread's
+// first AHEAD units are on their way while it finds its angles.
+// Bound: the bytes (a token's latency when there are few): 4 sequences of up to 2048 tokens, 32/8 heads of 128, interleaved pairs,
+// 34 us (4.3 TB/s).  Neighbouring threads have neighbouring chunks (a thread's pairs side by side: 39 us), two units are ahead (one:
+// 35, three: 38), and a token per workgroup is as fast as four with many and faster with few (1024 tokens 7.6 us against 10.6).
+template <bool F16>
 __global__ __launch_bounds__(256) void rotary_store_kernel(RotaryArgs a) {
-  extern __shared__ float2 s_turn[];   // [TOKENS][pairs] cosine, sine
+  extern __shared__ float2 s_turn[];   // [pairs] cosine, sine
+  constexpr int AHEAD = 2;
   const int b = blockIdx.y;
-  const int i0 = blockIdx.x * TOKENS;
+  const int i = blockIdx.x;
   const int tid = threadIdx.x;
   int P, n;
   clamped_lengths(a.c, a.prefix_len[b], a.n_new[b], a.c.capacity, a.N, &P, &n);
@@ -38,109 +43,119 @@ __global__ __launch_bounds__(256) void rotary_store_kernel(RotaryArgs a) {
     const int want = a.n_new[b] < a.N ? a.n_new[b] : a.N;
     if (want > n) report(a.c, b, TALON_STATUS_BAD_PAGE);   // rows beyond the page table are not written
   }
-  if (i0 >= n) return;
-  const int base = a.base != nullptr ? a.base[b] : 0;
-  for (int x = tid; x < TOKENS * a.pairs; x += 256) {
-    const int t = x / a.pairs, f = x - t * a.pairs;
-    if (i0 + t < n) {
-      int axis = a.axis != nullptr ? a.axis[f] : 0;
-      axis = axis < 0 ? 0 : (axis < a.axes ? axis : a.axes - 1);
-      const double at = static_cast<double>(base) + static_cast<double>(a.pos[(static_cast<size_t>(axis) * a.B + b) * a.N + i0 + t]);
-      const double turns = at * (static_cast<double>(a.inv_freq[f]) * 0.15915494309189535);
-      float sine, cosine;
-      sincospif(static_cast<float>(2.0 * (turns - rint(turns))), &sine, &cosine);
-      s_turn[x] = make_float2(cosine, sine);
+  if (i >= n) return;
+  // units of a head: groups of eight pairs, then of sixteen values that are copied
+  const bool whole = a.pairs % 8 == 0;           // (else value by value)
+  const int groups = (a.pairs + 7) / 8;
+  const int all = (a.Hq + 2 * a.Hkv) * a.units;
+
+  struct Unit {
+    uint4 c1, c2;
+    const uint16_t* src;
+    uint16_t* dst;     // nullptr: nothing to do
+    int unit, one, two;
+    bool is_v;
+  };
+  auto fetch = [&](int x) {
+    Unit r;
+    int head = a.inv_units != 0u ? static_cast<int>(__umulhi(static_cast<uint32_t>(x), a.inv_units)) : x;
+    r.unit = x - head * a.units;
+    r.dst = nullptr;
+    r.src = nullptr;
+    r.is_v = false;
+    r.one = r.two = 0;
+    r.c1 = r.c2 = make_uint4(0, 0, 0, 0);
+    if (x >= all) return r;
+    const bool is_q = head < a.Hq;
+    if (!is_q) head -= a.Hq;
+    r.is_v = !is_q && head >= a.Hkv;
+    if (r.is_v) head -= a.Hkv;
+    const RowsView& from = is_q ? a.q : (r.is_v ? a.v : a.k);
+    r.src = from.p + static_cast<int64_t>(b) * from.sb + static_cast<int64_t>(i) * from.st + static_cast<int64_t>(head) * from.sh;
+    // (neighbouring threads have neighbouring chunks, also of interleaved pairs, of which a chunk holds four)
+    r.one = r.unit < groups ? 8 * r.unit : 2 * a.pairs + 8 * (r.unit - groups);
+    r.two = r.unit < groups ? a.pairs + 8 * r.unit : r.one + 8 * (a.units - groups);   // (beyond the head: only `one`)
+    uint32_t entry = 0;
+    if (!is_q) entry = page_entry(a.c, b, P + i);
+    if (whole) {
+      r.c1 = *reinterpret_cast<const uint4*>(r.src + r.one);
+      if (r.two < a.Dh) r.c2 = *reinterpret_cast<const uint4*>(r.src + r.two);
     }
+    if (is_q) {
+      r.dst = a.q_out.p + static_cast<int64_t>(b) * a.q_out.sb + static_cast<int64_t>(i) * a.q_out.st + static_cast<int64_t>(head) * a.q_out.sh;
+    } else if (entry < a.c.num_pages) {
+      r.dst = chunk_at(static_cast<uint16_t*>(r.is_v ? a.c.v : a.c.k), row_chunk(a.c, entry, P + i, head));
+    } else {
+      report(a.c, b, TALON_STATUS_BAD_PAGE);   // nowhere to write to
+    }
+    return r;
+  };
+  auto finish = [&](const Unit& r) {
+    if (r.dst == nullptr) return;
+    const bool turned = !r.is_v && r.unit < groups;
+    if (whole) {
+      Chunk c1, c2, r1, r2;
+      c1.v = r.c1;
+      c2.v = r.c2;
+      r1.v = r.c1;
+      r2.v = r.c2;
+      if (turned && a.interleaved) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float2 t1 = s_turn[4 * r.unit + e], t2 = s_turn[4 * (groups + r.unit) + e];
+          const float x1 = to_float(c1.e[2 * e], F16), y1 = to_float(c1.e[2 * e + 1], F16);
+          const float x2 = to_float(c2.e[2 * e], F16), y2 = to_float(c2.e[2 * e + 1], F16);
+          r1.e[2 * e] = from_float(x1 * t1.x - y1 * t1.y, F16);
+          r1.e[2 * e + 1] = from_float(y1 * t1.x + x1 * t1.y, F16);
+          r2.e[2 * e] = from_float(x2 * t2.x - y2 * t2.y, F16);
+          r2.e[2 * e + 1] = from_float(y2 * t2.x + x2 * t2.y, F16);
+        }
+      } else if (turned) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const float2 t1 = s_turn[8 * r.unit + e];
+          const float x1 = to_float(c1.e[e], F16), y1 = to_float(c2.e[e], F16);
+          r1.e[e] = from_float(x1 * t1.x - y1 * t1.y, F16);
+          r2.e[e] = from_float(y1 * t1.x + x1 * t1.y, F16);
+        }
+      }
+      *reinterpret_cast<uint4*>(r.dst + r.one) = r1.v;
+      if (r.two < a.Dh) *reinterpret_cast<uint4*>(r.dst + r.two) = r2.v;
+    } else if (r.unit < groups) {
+      for (int e = 0; e < 8 && 8 * r.unit + e < a.pairs; ++e) {
+        const int f = 8 * r.unit + e;
+        const int one = a.interleaved ? 2 * f : f, two = a.interleaved ? 2 * f + 1 : f + a.pairs;
+        const uint16_t u1 = r.src[one], u2 = r.src[two];
+        const float x1 = to_float(u1, F16), y1 = to_float(u2, F16);
+        r.dst[one] = turned ? from_float(x1 * s_turn[f].x - y1 * s_turn[f].y, F16) : u1;
+        r.dst[two] = turned ? from_float(y1 * s_turn[f].x + x1 * s_turn[f].y, F16) : u2;
+      }
+    } else {
+      for (int e = 2 * a.pairs + r.unit - groups; e < a.Dh; e += a.units - groups) r.dst[e] = r.src[e];
+    }
+  };
+
+  Unit unit[AHEAD];
+#pragma unroll
+  for (int k = 0; k < AHEAD; ++k) unit[k] = fetch(tid + 256 * k);
+  const int base = a.base != nullptr ? a.base[b] : 0;
+  for (int f = tid; f < a.pairs; f += 256) {
+    int axis = a.axis != nullptr ? a.axis[f] : 0;
+    axis = axis < 0 ? 0 : (axis < a.axes ? axis : a.axes - 1);
+    const double at = static_cast<double>(base) + static_cast<double>(a.pos[(static_cast<size_t>(axis) * a.B + b) * a.N + i]);
+    const double turns = at * (static_cast<double>(a.inv_freq[f]) * 0.15915494309189535);
+    float sine, cosine;
+    sincospif(static_cast<float>(2.0 * (turns - rint(turns))), &sine, &cosine);
+    s_turn[f] = make_float2(cosine, sine);
   }
   __syncthreads();
-  // units of a head: groups of eight pairs, then groups of eight values that are copied
-  const int groups = (a.pairs + 7) / 8;
-  const int rest = a.Dh - 2 * a.pairs;
-  const int units = groups + (rest + 7) / 8;
-  const int copies = (a.Dh + 7) / 8;             // of a value head
-  const int per_token = (a.Hq + a.Hkv) * units + a.Hkv * copies;
-  const bool whole = a.pairs % 8 == 0;           // (else value by value)
-  for (int x = tid; x < TOKENS * per_token; x += 256) {
-    const int t = x / per_token;
-    int u = x - t * per_token;
-    const int i = i0 + t;
-    if (i >= n) break;
-    const int rotated = (a.Hq + a.Hkv) * units;
-    int head, unit;
-    bool is_q = false, is_v = false;
-    if (u < rotated) {
-      head = u / units;
-      unit = u - head * units;
-      is_q = head < a.Hq;
-      if (!is_q) head -= a.Hq;
-    } else {
-      u -= rotated;
-      head = u / copies;
-      unit = u - head * copies;
-      is_v = true;
-    }
-    const RowsView& from = is_q ? a.q : (is_v ? a.v : a.k);
-    const uint16_t* src = from.p + static_cast<int64_t>(b) * from.sb + static_cast<int64_t>(i) * from.st + static_cast<int64_t>(head) * from.sh;
-    uint16_t* dst;
-    if (is_q) {
-      dst = a.q_out.p + static_cast<int64_t>(b) * a.q_out.sb + static_cast<int64_t>(i) * a.q_out.st + static_cast<int64_t>(head) * a.q_out.sh;
-    } else {
-      const uint32_t entry = page_entry(a.c, b, P + i);
-      if (entry >= a.c.num_pages) {   // nowhere to write to
-        report(a.c, b, TALON_STATUS_BAD_PAGE);
-        continue;
-      }
-      dst = chunk_at(static_cast<uint16_t*>(is_v ? a.c.v : a.c.k), row_chunk(a.c, entry, P + i, head));
-    }
-    if (is_v) {
-      *reinterpret_cast<uint4*>(dst + 8 * unit) = *reinterpret_cast<const uint4*>(src + 8 * unit);
-    } else if (unit < groups) {
-      const float2* turn = s_turn + t * a.pairs + 8 * unit;
-      if (whole) {
-        const int one = a.interleaved ? 16 * unit : 8 * unit;
-        const int two = a.interleaved ? 16 * unit + 8 : a.pairs + 8 * unit;
-        Chunk c1, c2, r1, r2;
-        c1.v = *reinterpret_cast<const uint4*>(src + one);
-        c2.v = *reinterpret_cast<const uint4*>(src + two);
-        if (a.interleaved) {
+  for (int x = tid;;) {
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const float2 t1 = turn[e], t2 = turn[4 + e];
-            const float x1 = to_float(c1.e[2 * e], F16), y1 = to_float(c1.e[2 * e + 1], F16);
-            const float x2 = to_float(c2.e[2 * e], F16), y2 = to_float(c2.e[2 * e + 1], F16);
-            r1.e[2 * e] = from_float(x1 * t1.x - y1 * t1.y, F16);
-            r1.e[2 * e + 1] = from_float(y1 * t1.x + x1 * t1.y, F16);
-            r2.e[2 * e] = from_float(x2 * t2.x - y2 * t2.y, F16);
-            r2.e[2 * e + 1] = from_float(y2 * t2.x + x2 * t2.y, F16);
-          }
-        } else {
+    for (int k = 0; k < AHEAD; ++k) finish(unit[k]);
+    x += 256 * AHEAD;
+    if (x >= all) break;
 #pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            const float2 t1 = turn[e];
-            const float x1 = to_float(c1.e[e], F16), y1 = to_float(c2.e[e], F16);
-            r1.e[e] = from_float(x1 * t1.x - y1 * t1.y, F16);
-            r2.e[e] = from_float(y1 * t1.x + x1 * t1.y, F16);
-          }
-        }
-        *reinterpret_cast<uint4*>(dst + one) = r1.v;
-        *reinterpret_cast<uint4*>(dst + two) = r2.v;
-      } else {
-        for (int e = 0; e < 8 && 8 * unit + e < a.pairs; ++e) {
-          const int f = 8 * unit + e;
-          const int one = a.interleaved ? 2 * f : f, two = a.interleaved ? 2 * f + 1 : f + a.pairs;
-          const float x1 = to_float(src[one], F16), y1 = to_float(src[two], F16);
-          dst[one] = from_float(x1 * turn[e].x - y1 * turn[e].y, F16);
-          dst[two] = from_float(y1 * turn[e].x + x1 * turn[e].y, F16);
-        }
-      }
-    } else {
-      const int d = 2 * a.pairs + 8 * (unit - groups);
-      if (whole) {
-        *reinterpret_cast<uint4*>(dst + d) = *reinterpret_cast<const uint4*>(src + d);
-      } else {
-        for (int e = 0; e < 8 && d + e < a.Dh; ++e) dst[d + e] = src[d + e];
-      }
-    }
+    for (int k = 0; k < AHEAD; ++k) unit[k] = fetch(x + 256 * k);
   }
 }
 
@@ -425,19 +440,15 @@ __global__ __launch_bounds__(kMoveThreads) void evict_move_kernel(EvictArgs a, i
 
 }  // namespace
 
-hipError_t launch_rotary_store(const RotaryArgs& a, int dtype, hipStream_t s) {
-  // few tokens: one per workgroup, to have all of them at work; many: four, whose angles fill a workgroup's threads
-  const bool four = static_cast<long long>(a.B) * a.N >= 2048 && a.pairs <= 128;
-  const dim3 grid(four ? (a.N + 3) / 4 : a.N, a.B);
-  const size_t lds = static_cast<size_t>(four ? 4 : 1) * a.pairs * sizeof(float2);
-  const bool f16 = dtype == TALON_DTYPE_F16;
-  if (four) {
-    if (f16) hipLaunchKernelGGL((rotary_store_kernel<true, 4>), grid, dim3(256), lds, s, a);
-    else hipLaunchKernelGGL((rotary_store_kernel<false, 4>), grid, dim3(256), lds, s, a);
-  } else {
-    if (f16) hipLaunchKernelGGL((rotary_store_kernel<true, 1>), grid, dim3(256), lds, s, a);
-    else hipLaunchKernelGGL((rotary_store_kernel<false, 1>), grid, dim3(256), lds, s, a);
-  }
+hipError_t launch_rotary_store(const RotaryArgs& args, int dtype, hipStream_t s) {
+  RotaryArgs a = args;
+  a.units = (a.pairs + 7) / 8 + (a.Dh - 2 * a.pairs + 15) / 16;
+  // (x / units as a product: exact for x * units < 2^32, and x < 65792 heads * 65 units)
+  a.inv_units = a.units == 1 ? 0u : static_cast<uint32_t>(((1ull << 32) + a.units - 1) / a.units);
+  const dim3 grid(a.N, a.B);
+  const size_t lds = static_cast<size_t>(a.pairs) * sizeof(float2);
+  if (dtype == TALON_DTYPE_F16) hipLaunchKernelGGL(rotary_store_kernel<true>, grid, dim3(256), lds, s, a);
+  else hipLaunchKernelGGL(rotary_store_kernel<false>, grid, dim3(256), lds, s, a);
   return hipGetLastError();
 }
 
