@@ -17,15 +17,30 @@ struct PagedPlan {
   size_t off_m, off_l, off_cut, bytes;   // workspace: outputs, maxima, denominators, cuts
 };
 
+// Which kernel, and how the key tiles of all row tiles are cut into shares (times in us, bf16, heads of 128, 32/8 heads where not
+// said otherwise, P rows in the cache):
+//   few rows    up to 32 (token, head) rows of a KV head: the wavefronts of a workgroup share the keys of one row tile.  The other
+//               kernel, a row tile of 32 rows per wavefront, would leave three quarters of a workgroup without rows.
+//   wavefronts  8 from 512 rows on (a K/V tile is read once for 256 rows): a chunk of 2048 512 against 538 with 4, 4 trees of 128
+//               nodes 59 against 64; 60 nodes (240 rows) 26.7 against 24.5.  Heads of 256 have registers for 4 only.
+//   whole       prefixes of at most that many key tiles are not cut: few rows, 1 x 1000 rows cut 13.2 whole 14.6, but 8 x 1024
+//               18.5 and 17.4, and 500 rows 11.2 whole.
+//   least       key tiles that a share has at least; a tree of 60 nodes at P = 2048: 2 24.5, 4 22.5, 8 26.3 (few sequences get
+//               even pieces instead, below).
+//   pieces      most even pieces of a row tile when there are few: one token at P = 2048 8 15.8, 16 14.9, 24 14.7, 32 14.8; at
+//               P = 8192 22.3, 20.9, 19.8, 20.7; at P = 32768 62, 43, 39.3, 38.8.
+//   extra       what a row tile costs besides its tiles (queries, last stores, partial results), in tiles: 2048 tokens 0 488, 4 479,
+//               6 471; 4 trees 65.6, 56, 57.8; few rows, 64 sequences of up to 1024 rows 0 59.3, 4 51, 8 47.1, 16 45.5, and 32 of 4
+//               tokens at P = 2048 52, 48.9, 47.7, 49.3.  Attention weights join nothing: half of that.
 constexpr int kPagedTile = 64;
-constexpr int kPagedWholeTiles = 4;   // up to so many key tiles a row tile is not cut
-constexpr int kPagedLeast = 2;        // fewest key tiles of a share
-constexpr int kPagedFewTile = 32;     // the same for few rows
+constexpr int kPagedWholeTiles = 4;
+constexpr int kPagedLeast = 2;
+constexpr int kPagedExtra = 5;
+constexpr int kPagedFewTile = 32;
 constexpr int kPagedFewWhole = 24;
 constexpr int kPagedFewLeast = 8;
-constexpr int kPagedPieces = 24;
-constexpr int kPagedExtra = 5;
 constexpr int kPagedFewExtra = 8;
+constexpr int kPagedPieces = 24;
 constexpr int kWeighExtra = 4;
 
 inline PagedPlan paged_plan(int B, int N, int Hq, int Hkv, int Dh, int max_prefix_len) {
@@ -48,7 +63,8 @@ inline PagedPlan paged_plan(int B, int N, int Hq, int Hkv, int Dh, int max_prefi
     return p;
   }
   const long long slots = few ? (Dh == 64 ? 512 : 256) : (p.waves == 8 || Dh == 256 ? 256 : 512);   // workgroups that the device holds at once
-  // Few row tiles: as many pieces of each as there are workgroups for, up to what the join reads in three rounds.
+  // Few row tiles (an eighth of the workgroups): even pieces of each, as many as there are workgroups for, up to what the join reads in
+  // three rounds; 8 ragged sequences of up to 8192 rows (a quarter) are better off in equal shares, 45.8 against 50.4.
   p.least = few ? kPagedFewLeast : kPagedLeast;
   if (items * 8 <= slots) {
     const long long pieces = slots / items < kPagedPieces ? slots / items : kPagedPieces;
