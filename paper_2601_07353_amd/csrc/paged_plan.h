@@ -62,7 +62,7 @@ inline PagedPlan paged_plan(int B, int N, int Hq, int Hkv, int Dh, int max_prefi
     p.bytes = 256;   // nothing is staged, keep a token size
     return p;
   }
-  const long long slots = few ? (Dh == 64 ? 512 : 256) : (p.waves == 8 || Dh == 256 ? 256 : 512);   // workgroups that the device holds at once
+  const long long slots = few ? 256 : (p.waves == 8 || Dh == 256 ? 256 : 512);   // workgroups that the device holds at once
   // Few row tiles (an eighth of the workgroups): even pieces of each, as many as there are workgroups for, up to what the join reads in
   // three rounds; 8 ragged sequences of up to 8192 rows (a quarter) are better off in equal shares, 45.8 against 50.4.
   p.least = few ? kPagedFewLeast : kPagedLeast;
@@ -93,7 +93,7 @@ inline WeighPlan weigh_plan(int B, int Hkv, int Dh, int rows) {
   p.least = kPagedFewLeast;
   p.extra = kWeighExtra;
   p.tiles = items * (most + p.extra);
-  const long long slots = Dh == 64 ? 512 : 256, enough = (p.tiles + p.least - 1) / p.least + items;
+  const long long slots = 256, enough = (p.tiles + p.least - 1) / p.least + items;
   p.slots = static_cast<int>(enough < slots ? enough : slots);
   return p;
 }
