@@ -653,7 +653,7 @@ __global__ __launch_bounds__(64 * NW, DH == 256 ? 1 : (NW == 4 ? 2 : 1)) void pa
     if (seen_from <= 0) whole_from = 0;
     whole_from = whole_from < t_begin ? t_begin : whole_from;
     whole_to = whole_to < t_end ? whole_to : t_end;
-    if (whole_from >= whole_to || DH == 256) whole_from = whole_to = t_end;   // none (or no registers for two tiles' scores)
+    if (whole_from >= whole_to) whole_from = whole_to = t_end;   // none
     auto stage_of = [&](int t) { return (t - whole_from) & 1; };
 
     // ---- prologue.  Two round trips to memory: everything that needs no other load (queries, page entries, positions, slopes, mask
@@ -699,7 +699,7 @@ __global__ __launch_bounds__(64 * NW, DH == 256 ? 1 : (NW == 4 ? 2 : 1)) void pa
     tile_landed();
     for (int t = t_begin; t < t_end; ++t) {
       floatx16 s_a[2];
-      const bool whole_run = DH != 256 && t == whole_from;
+      const bool whole_run = t == whole_from;
       if (!whole_run) clean_v(t, stage_of(t));
       if (works) {
         qk(stage_k(stage_of(t)), s_a, lane_again());
