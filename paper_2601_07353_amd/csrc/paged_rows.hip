@@ -15,6 +15,8 @@ __device__ __forceinline__ uint16_t from_float(float v, bool f16) {
   return __builtin_bit_cast(uint16_t, static_cast<__bf16>(v));
 }
 
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
 union Chunk {
   uint4 v;
   uint16_t e[8];
@@ -215,6 +217,7 @@ __global__ __launch_bounds__(256) void paged_compact_kernel(CompactArgs a) {
     w_moves = node >= 0 && node < a.N && node != tid && P + node < a.weight_rows && P + tid < a.weight_rows;
     if (w_moves) w = row[P + node];
   }
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // (all have arrived before one is written over)
   __syncthreads();
 #pragma unroll
   for (int u = 0; u < kPer; ++u)
@@ -378,14 +381,19 @@ __global__ __launch_bounds__(kSelectThreads) void evict_select_kernel(EvictArgs 
 // ---- rows move: kept[m] of the source's pages to row m of the destination's.
 // In place a workgroup has one (sequence, KV head) and 2^lanes_log chunks of 8 values of the rows of K or of V and goes through the
 // rows in order, a block of them read before it is written (a row only moves towards the front, so nothing is read behind its
-// write).  Into other pages there is no order, and the rows are spread over as many workgroups as there are blocks.
+// write).  Into other pages there is no order, and the rows are spread over as many workgroups as there are blocks.  A thread finds one
+// row's places for all, while the block before moves.
 // Bound: the bytes; 16 sequences, 4096 of up to 16384 rows each (8 heads of 128) into other pages 107 to 118 us (5 TB/s).  One
-// sequence in place has too few workgroups for that: 1024 of 4096 rows 7 us, 30000 of 65536 about 190.
+// sequence in place has too few workgroups for that: 1024 of 4096 rows 6.5 us, 30000 of 65536 183 us (203 where every lane finds its
+// rows itself and between the blocks).
 constexpr int kMoveThreads = 1024;
 constexpr int kMoveChunks = 8;   // of 16 bytes per thread and block
 __global__ __launch_bounds__(kMoveThreads) void evict_move_kernel(EvictArgs a, int lanes_log) {
+  constexpr uint32_t kStays = ~0u;
+  __shared__ uint2 s_row[2][kMoveThreads];   // where a block's rows lie and where they go (first chunks), or kStays
   const int tid = threadIdx.x;
   const int per = kMoveThreads >> lanes_log;                       // rows of a chunk of the block
+  const int step = per * kMoveChunks;                              // rows of a block: at most one per thread
   const int groups = (a.Dh / 8 + (1 << lanes_log) - 1) >> lanes_log;
   const int unit = blockIdx.x;                                     // K or V, a group of chunks
   const bool is_v = unit >= groups;
@@ -401,40 +409,64 @@ __global__ __launch_bounds__(kMoveThreads) void evict_move_kernel(EvictArgs a, i
   const int32_t* const kept = a.kept + (static_cast<size_t>(b) * a.Hkv + g) * a.budget;
   const uint16_t* const from = static_cast<const uint16_t*>(is_v ? a.src.v : a.src.k);
   uint16_t* const to = static_cast<uint16_t*>(is_v ? a.dst.v : a.dst.k);
-  const int step = per * kMoveChunks;
-  for (int m0 = static_cast<int>(blockIdx.y) * step; m0 < room; m0 += static_cast<int>(gridDim.y) * step) {
-    uint4 v[kMoveChunks];
-    int row[kMoveChunks];
-    uint32_t e_from[kMoveChunks], e_to[kMoveChunks];
-#pragma unroll
-    for (int u = 0; u < kMoveChunks; ++u) {
-      const int m = m0 + (tid >> lanes_log) + per * u;
-      row[u] = kept[m < room ? m : room - 1];
-      e_to[u] = page_entry(a.dst, b, m < room ? m : room - 1);
+  const int stride = static_cast<int>(gridDim.y) * step;
+  int m0 = static_cast<int>(blockIdx.y) * step;
+  if (m0 >= room) return;
+
+  // This thread's row of the block that begins at `first`, in two round trips to memory and then to LDS.
+  int row = 0, m = 0;
+  uint32_t e_from = 0, e_to = 0;
+  bool mine = false;
+  auto load_row = [&](int first) {
+    m = first + tid;
+    mine = tid < step && m < room;
+    if (mine) row = kept[m];
+  };
+  auto load_pages = [&]() {
+    if (mine) {
+      e_from = page_entry(a.src, b, row);
+      e_to = page_entry(a.dst, b, m);
     }
-#pragma unroll
-    for (int u = 0; u < kMoveChunks; ++u) e_from[u] = page_entry(a.src, b, row[u]);
+  };
+  auto place = [&](int st) {
+    uint2 at = make_uint2(kStays, kStays);
+    if (mine && !(a.in_place && row == m)) {
+      if (e_from < a.src.num_pages && e_to < a.dst.num_pages) at = make_uint2(row_chunk(a.src, e_from, row, g), row_chunk(a.dst, e_to, m, g));
+      else report(e_from < a.src.num_pages ? a.dst : a.src, b, TALON_STATUS_BAD_PAGE);
+    }
+    s_row[st][tid] = at;
+  };
+  load_row(m0);
+  load_pages();
+  place(0);
+  __syncthreads();
+  for (int st = 0; m0 < room; m0 += stride, st ^= 1) {
+    const bool more = m0 + stride < room;
+    if (more) load_row(m0 + stride);
+    u32x4 v[kMoveChunks];
     uint32_t dest[kMoveChunks];
-    uint32_t moved = 0;
 #pragma unroll
     for (int u = 0; u < kMoveChunks; ++u) {
-      const int m = m0 + (tid >> lanes_log) + per * u;
-      v[u] = make_uint4(0, 0, 0, 0);
-      dest[u] = 0;
-      if (m < room && col * 8 < a.Dh && !(a.in_place && row[u] == m)) {
-        if (e_from[u] < a.src.num_pages && e_to[u] < a.dst.num_pages) {
-          v[u] = *reinterpret_cast<const uint4*>(chunk_at(from, row_chunk(a.src, e_from[u], row[u], g) + col));
-          dest[u] = row_chunk(a.dst, e_to[u], m, g) + col;
-          moved |= 1u << u;
-        } else {
-          report(e_from[u] < a.src.num_pages ? a.dst : a.src, b, TALON_STATUS_BAD_PAGE);
-        }
+      const uint2 at = s_row[st][(tid >> lanes_log) + per * u];
+      v[u] = u32x4{0, 0, 0, 0};
+      dest[u] = kStays;
+      if (at.y != kStays && col * 8 < a.Dh) {
+        v[u] = *reinterpret_cast<const u32x4*>(chunk_at(from, at.x + col));
+        dest[u] = at.y + col;
       }
     }
+    if (more) load_pages();
+    // (all rows of the block have arrived before one is written over)
+#pragma unroll
+    for (int u = 0; u < kMoveChunks; ++u) asm volatile("" : "+v"(v[u]));
     if (a.in_place) __syncthreads();
 #pragma unroll
     for (int u = 0; u < kMoveChunks; ++u)
-      if (moved >> u & 1u) *reinterpret_cast<uint4*>(chunk_at(to, dest[u])) = v[u];
+      if (dest[u] != kStays) *reinterpret_cast<u32x4*>(chunk_at(to, dest[u])) = v[u];
+    if (more) {
+      place(st ^ 1);
+      __syncthreads();
+    }
   }
 }
 
@@ -465,10 +497,9 @@ hipError_t launch_paged_evict(const EvictArgs& a, hipStream_t s) {
   const int most = a.budget < a.max_len ? a.budget : a.max_len;
   if (most == 0) return hipSuccess;
   // Chunks of a row that a workgroup moves: 128 values or what the head has (2 KiB that are read together and whole lines).  In place,
-  // where a workgroup has all rows, 64 values if that leaves fewer workgroups than compute units: 4 sequences, 2048 of 8192 rows 25.9 us
-  // against 31.0; with 16 sequences 128 values are better, 4096 of 16384 rows 132 us against 140 (32 values: 189).
-  int lanes_log = 1;
-  while (lanes_log < 4 && (8 << lanes_log) < a.Dh) ++lanes_log;
+  // where a workgroup has all rows, 64 values if that leaves fewer workgroups than compute units: 4 sequences, 2048 of 8192 rows 25.8 us
+  // against 28.5, one sequence, 30000 of 65536 233 against 321; with 16 sequences 128 values are better, 4096 of 16384 rows 129 us against 136.
+  int lanes_log = a.Dh > 64 ? 4 : 3;
   if (a.in_place && lanes_log == 4 && 2ll * a.B * a.Hkv * ((a.Dh + 127) / 128) < 256) lanes_log = 3;
   const int step = (kMoveThreads >> lanes_log) * kMoveChunks;
   const int groups = (a.Dh / 8 + (1 << lanes_log) - 1) >> lanes_log;
