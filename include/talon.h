@@ -540,8 +540,8 @@ typedef struct talon_scores {
  * with x1 = x[f], x2 = x[f + pairs], or, interleaved, x1 = x[2f], x2 = x[2f + 1]; values from 2*pairs on and all
  * of v are copied.  axis(f) = pair_axis[f] clamped to [0, axes) (NULL: 0): positions in time, height and width of
  * an image's tokens each turn their own pairs.
- *   q, q_out [B][N][Hq][Dh] (q_out may be q: each value is read and written by one thread), k, v [B][N][Hkv][Dh];
- *   views of one fused tensor are fine.  pos int32 [axes][B][N]; pos_base int32 [B] or NULL; inv_freq float [pairs].
+ *   q, q_out [B][N][Hq][Dh] (q_out may be q, with q's strides: each value is read and written by one thread), k, v
+ *   [B][N][Hkv][Dh]; views of one fused tensor are fine.  pos int32 [axes][B][N]; pos_base int32 [B] or NULL; inv_freq float [pairs].
  *   Tokens i >= n_new[b] are neither read nor written.  Positions are taken in 64 bits, sines and cosines are
  *   good to fp32, results are rounded once.
  *   Errors: INVALID_ARG, UNSUPPORTED (dtype, sizes).

@@ -127,6 +127,7 @@ int talon_rotary_store(const talon_paged_cache* cache, const talon_view* q, cons
   if ((rc = check_view(k, "k", B, N, Hkv, Dh, false, &a.k))) return rc;
   if ((rc = check_view(v, "v", B, N, Hkv, Dh, false, &a.v))) return rc;
   if ((rc = check_view(q_out, "q_out", B, N, Hq, Dh, true, &a.q_out))) return rc;
+  if (a.q.p == a.q_out.p && (a.q.sb != a.q_out.sb || a.q.st != a.q_out.st || a.q.sh != a.q_out.sh)) { set_error("q in place needs q's strides"); return TALON_ERR_INVALID_ARG; }
   if (pairs < 0 || pairs > Dh / 2) { set_error("pairs=%d outside [0, Dh/2=%d]", pairs, Dh / 2); return TALON_ERR_INVALID_ARG; }
   if (axes < 1 || axes > 8) { set_error("axes=%d outside [1, 8]", axes); return TALON_ERR_INVALID_ARG; }
   if (pairs > 0 && (!pos || !inv_freq)) { set_error("pos / inv_freq is NULL"); return TALON_ERR_INVALID_ARG; }

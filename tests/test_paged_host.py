@@ -112,6 +112,7 @@ def test_what_else_is_refused(lib):
             ("store", dict(o=view(sh=0)), INVALID, "q_out: strides"), ("store", dict(k=view(data=0)), INVALID, "k is NULL"), ("store", dict(v=view(st=3)), INVALID, "v: strides"),
             ("store", dict(pairs=65), INVALID, "pairs=65"), ("store", dict(pairs=-1), INVALID, "pairs"), ("store", dict(axes=0), INVALID, "axes"), ("store", dict(axes=9), INVALID, "axes"),
             ("store", dict(pos=None), INVALID, "pos"), ("store", dict(freq=None), INVALID, "inv_freq"), ("store", dict(base=P + 1), INVALID, "misaligned"),
+            ("store", dict(q=view(sh=256)), INVALID, "in place"), ("store", dict(o=view(st=8192)), INVALID, "in place"),
             ("attend", dict(o=view(st=0)), INVALID, "out: strides"), ("attend", dict(lse=P + 1), INVALID, "out_lse"), ("attend", dict(ws=None), INVALID, "workspace"),
             ("attend", dict(ws=P + 8), INVALID, "workspace"), ("attend", dict(nb=1000), WORKSPACE, "smaller"),
             ("weigh", dict(lse=None), INVALID, "lse"), ("weigh", dict(w=None), INVALID, "weights"), ("weigh", dict(prior=P + 2), INVALID, "misaligned"),
