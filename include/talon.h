@@ -561,7 +561,7 @@ int talon_rotary_store(const talon_paged_cache* cache, const talon_view* q, cons
  *   rows are cut depends on all lengths of the batch: the low bits of a sequence's result may differ between
  *   batches.  The same call on the same data repeats its result bit for bit.
  *   `workspace`: talon_paged_attention_workspace_bytes bytes, no initialisation needed, not to be shared by calls that
- *   run at the same time.
+ *   run at the same time.  The bytes for one max_prefix_len hold for every smaller one (same B, N, heads) and any page table.
  *   Errors: INVALID_ARG, UNSUPPORTED (Dh other than 64, 128, 256; Hq % Hkv != 0; Hq/Hkv > 128; more than 2^30 key
  *   tiles), WORKSPACE.
  */

@@ -145,7 +145,7 @@ size_t talon_paged_attention_workspace_bytes(int32_t B, int32_t N, int32_t Hq, i
   if (max_prefix_len < 0 || max_prefix_len > kMostRows) { set_error("max_prefix_len=%d outside [0, %d]", max_prefix_len, kMostRows); return 0; }
   const PagedPlan p = paged_plan(B, N, Hq, Hkv, Dh, max_prefix_len);
   if (p.tiles >= 1ll << 30) { set_error("%lld key tiles are more than one call takes", p.tiles); return 0; }
-  return p.bytes;
+  return p.room;
 }
 
 int talon_paged_attention(const talon_paged_cache* cache, const talon_view* q, int32_t N, int32_t Hq, const int32_t* n_new,

@@ -15,6 +15,7 @@ struct PagedPlan {
   int rows_slot;    // rows of a partial result
   long long tiles;  // key tiles of the call if every sequence is as long as it may be
   size_t off_m, off_l, off_cut, bytes;   // workspace: outputs, maxima, denominators, cuts
+  size_t room;      // a workspace that holds this plan and the plans of all shorter prefixes
 };
 
 // Which kernel, and how the key tiles of all row tiles are cut into shares (times in us, bf16, heads of 128, 32/8 heads where not
@@ -59,26 +60,37 @@ inline PagedPlan paged_plan(int B, int N, int Hq, int Hkv, int Dh, int max_prefi
   if (!p.split) {
     p.slots = static_cast<int>(items < (1ll << 30) ? items : (1ll << 30));
     p.least = 1;
-    p.bytes = 256;   // nothing is staged, keep a token size
+    p.bytes = p.room = 256;   // nothing is staged, keep a token size
     return p;
   }
   const long long slots = few ? 256 : (p.waves == 8 || Dh == 256 ? 256 : 512);   // workgroups that the device holds at once
   // Few row tiles (an eighth of the workgroups): even pieces of each, as many as there are workgroups for, up to what the join reads in
   // three rounds; 8 ragged sequences of up to 8192 rows (a quarter) are better off in equal shares, 45.8 against 50.4.
-  p.least = few ? kPagedFewLeast : kPagedLeast;
+  const int base = few ? kPagedFewLeast : kPagedLeast;
+  p.least = base;
+  // Longer prefixes do not always take more workgroups: even pieces get larger, and what a row tile costs besides its tiles (`extra`)
+  // weighs less.  With least >= base the number `enough` below is at most what `base` gives, which grows with the
+  // prefix; with least >= most / pieces it is at most items * (pieces + extra / base + 1), whatever the prefix.
+  long long bound = (p.tiles + base - 1) / base + items;
   if (items * 8 <= slots) {
     const long long pieces = slots / items < kPagedPieces ? slots / items : kPagedPieces;
+    const long long even_bound = items * (pieces + (p.extra + base - 1) / base + 1);
+    bound = bound < even_bound ? bound : even_bound;
     const long long even = (most + pieces - 1) / pieces;
     p.least = static_cast<int>(even > p.least ? even : p.least);
   }
   const long long enough = (p.tiles + p.least - 1) / p.least + items;   // (also as even pieces of the row tiles)
   p.slots = static_cast<int>(enough < slots ? enough : slots);
-  const size_t slot_rows = 2 * static_cast<size_t>(p.slots) * p.rows_slot;
   auto up = [](size_t x) { return (x + 255) / 256 * 256; };
-  p.off_m = up(slot_rows * Dh * sizeof(float));
-  p.off_l = p.off_m + up(slot_rows * sizeof(float));
-  p.off_cut = p.off_l + up(slot_rows * sizeof(float));
-  p.bytes = p.off_cut + up(static_cast<size_t>(p.slots) * 16);
+  auto lay_out = [&](long long n) {   // of n workgroups
+    const size_t slot_rows = 2 * static_cast<size_t>(n) * p.rows_slot;
+    p.off_m = up(slot_rows * Dh * sizeof(float));
+    p.off_l = p.off_m + up(slot_rows * sizeof(float));
+    p.off_cut = p.off_l + up(slot_rows * sizeof(float));
+    return p.off_cut + up(static_cast<size_t>(n) * 16);
+  };
+  p.room = lay_out(bound < slots ? bound : slots);
+  p.bytes = lay_out(p.slots);
   return p;
 }
 
