@@ -488,7 +488,7 @@ int talon_tree_attention_static(const void* q, const void* k_prefix, const void*
  * What only the device can see: a table entry outside [0, num_pages), where a row of it is read or written,
  * and rows beyond the table's max_pages * page_size set TALON_STATUS_BAD_PAGE in status[b].  Nothing outside the
  * pool is touched; rows that have no place are not written, and a sequence's outputs are not meaningful where
- * a row of it could not be read.  Lengths outside their bounds are taken as the nearest bound.  No call clears
+ * a row of it could not be read; a new token without a row gets no output.  Lengths outside their bounds are taken as the nearest bound.  No call clears
  * status.
  */
 typedef struct talon_paged_cache {

@@ -136,7 +136,9 @@ __device__ __forceinline__ bool find_share(const PagedAttnArgs& a, int lane, Sha
   auto look = [&](int bb) {
     sum = pieces = P = n = 0;
     if (bb < a.B) {
-      clamped_lengths(a.c, sc.prefix_len[bb], sc.n_new[bb], sc.max_prefix_len, sc.N, &P, &n);
+      const int prefix = sc.prefix_len[bb], fresh = sc.n_new[bb];
+      clamped_lengths(a.c, prefix, fresh, sc.max_prefix_len, sc.N, &P, &n);
+      if (share == 0 && threadIdx.x < 64) report_table_end(a.c, bb, prefix, fresh, sc.max_prefix_len, sc.N);
       const int row_tiles = ALL ? (P + n > 0 ? 1 : 0) : (n * a.G + ROW_TILE - 1) / ROW_TILE;
       if (!split) sum = row_tiles;
       else {

@@ -28,6 +28,13 @@ __device__ __forceinline__ void clamped_lengths(const PagedRows& c, int prefix, 
 
 __device__ __forceinline__ void report(const PagedRows& c, int b, uint32_t bit) { atomicOr(&c.status[b], bit); }
 
+// Rows that lie beyond the page table, which clamped_lengths leaves out: reported by one thread of a call.
+__device__ __forceinline__ void report_table_end(const PagedRows& c, int b, int prefix, int fresh, int max_prefix, int N) {
+  const int p = prefix < 0 ? 0 : (prefix > max_prefix ? max_prefix : prefix);
+  const int m = fresh < 0 ? 0 : (fresh > N ? N : fresh);
+  if (p + m > c.capacity) report(c, b, TALON_STATUS_BAD_PAGE);
+}
+
 // First chunk of (row's page entry, row, KV head); an entry that names no page of the pool is page 0 (the caller reports it).
 __device__ __forceinline__ uint32_t row_chunk(const PagedRows& c, uint32_t entry, int row, int g) {
   const uint32_t page = entry < c.num_pages ? entry : 0u;

@@ -265,6 +265,7 @@ __global__ __launch_bounds__(kSelectThreads) void evict_select_kernel(EvictArgs 
   int len = a.len[b];
   for (int i = tid; i < 3 * 2048; i += kSelectThreads) (&s_count[0][0])[i] = 0u;
   len = len < 0 ? 0 : (len < a.max_len ? len : a.max_len);
+  if (len > a.src.capacity && g == 0 && tid == 0) report(a.src, b, TALON_STATUS_BAD_PAGE);   // rows beyond the page table
   len = len < a.src.capacity ? len : a.src.capacity;
   const float* const w = a.weights + static_cast<size_t>(b) * a.stride_b + static_cast<size_t>(g) * a.stride_h;
   float* const w_out = a.new_weights != nullptr ? a.new_weights + static_cast<size_t>(b) * a.new_stride_b + static_cast<size_t>(g) * a.new_stride_h : nullptr;

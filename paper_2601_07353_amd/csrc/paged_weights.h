@@ -140,6 +140,7 @@ __global__ __launch_bounds__(512, DH == 256 ? 2 : 4) void paged_weights_kernel(P
   const int b = blockIdx.z, g = blockIdx.y;
   int P, n;
   clamped_lengths(a.c, sc.prefix_len[b], sc.n_new[b], sc.max_prefix_len, sc.N, &P, &n);
+  if (blockIdx.x == 0 && g == 0 && threadIdx.x == 0) report_table_end(a.c, b, sc.prefix_len[b], sc.n_new[b], sc.max_prefix_len, sc.N);
   const int len = P + n;
   const int key0 = static_cast<int>(blockIdx.x) * kWeighRows;
   if (key0 >= len) return;
