@@ -557,7 +557,8 @@ int talon_rotary_store(const talon_paged_cache* cache, const talon_view* q, cons
  *   q, out [B][N][Hq][Dh]; out_lse float [B][N][Hq] or NULL: natural-log softmax denominator.  Rows i >= n_new[b]
  *   of out and out_lse are untouched.  prefix_len[b] <= max_prefix_len (host bound, sizes the launch).
  *   Arithmetic: matrix instructions with fp32 accumulation, fp32 online softmax, probabilities rounded to the
- *   storage type before the product with V, outputs rounded once (partial results of a row are fp32).  Where
+ *   storage type before the product with V, outputs rounded once (partial results of a row are fp32).  Capped scores
+ *   are off by up to 2^-22 of the cap where it is at most 64; larger caps are formed to fp32 accuracy, in more time.  Where
  *   rows are cut depends on all lengths of the batch: the low bits of a sequence's result may differ between
  *   batches.  The same call on the same data repeats its result bit for bit.
  *   `workspace`: talon_paged_attention_workspace_bytes bytes, no initialisation needed, not to be shared by calls that

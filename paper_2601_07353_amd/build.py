@@ -16,7 +16,7 @@ MARSHAL_PATH = os.path.join(LIB_DIR, "_talon_marshal.so")
 OBJ_DIR = os.path.join(PKG, "_build")
 
 SOURCES = ["api.hip", "expand.hip", "ahead.hip", "select.hip", "literal.hip", "attention.hip", "accept.hip", "calibrate.hip",
-           "paged_api.hip", *["paged_attention_%s_%d.hip" % (t, d) for d in (128, 64, 256) for t in ("bf16", "f16")], "paged_weights_bf16.hip", "paged_weights_f16.hip", "paged_rows.hip"]
+           "paged_attention_bf16_far.hip", "paged_attention_f16_far.hip", "paged_api.hip", *["paged_attention_%s_%d.hip" % (t, d) for d in (128, 64, 256) for t in ("bf16", "f16")], "paged_weights_bf16.hip", "paged_weights_f16.hip", "paged_rows.hip"]
 
 FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",

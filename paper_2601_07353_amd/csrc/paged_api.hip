@@ -99,7 +99,7 @@ int check_scores(const talon_scores* s, int N, int Dh, int max_prefix_len, const
   out->N = N; out->words = (N + 63) / 64; out->max_prefix_len = max_prefix_len; out->window = s->window;
   out->scale_log2e = static_cast<float>(scale * log2e);
   out->cap_log2e = static_cast<float>(s->softcap * log2e);
-  out->cap_in = s->softcap > 0.f ? static_cast<float>(weights ? scale / s->softcap : 2.0 * scale * log2e / s->softcap) : 0.f;
+  out->cap_in = s->softcap > 0.f ? static_cast<float>(weights || s->softcap > kNearCap ? scale / s->softcap : 2.0 * scale * log2e / s->softcap) : 0.f;
   return TALON_OK;
 }
 
@@ -180,7 +180,8 @@ int talon_paged_attention(const talon_paged_cache* cache, const talon_view* q, i
   const hipStream_t s = static_cast<hipStream_t>(stream);
   const bool f16 = cache->dtype == TALON_DTYPE_F16;
   hipError_t e;
-  if (Dh == 64) e = f16 ? launch_paged_attention_f16_64(a, p.waves, s) : launch_paged_attention_bf16_64(a, p.waves, s);
+  if (scores && scores->softcap > kNearCap) e = f16 ? launch_paged_attention_f16_far(a, Dh, p.waves, s) : launch_paged_attention_bf16_far(a, Dh, p.waves, s);
+  else if (Dh == 64) e = f16 ? launch_paged_attention_f16_64(a, p.waves, s) : launch_paged_attention_bf16_64(a, p.waves, s);
   else if (Dh == 128) e = f16 ? launch_paged_attention_f16_128(a, p.waves, s) : launch_paged_attention_bf16_128(a, p.waves, s);
   else e = f16 ? launch_paged_attention_f16_256(a, p.waves, s) : launch_paged_attention_bf16_256(a, p.waves, s);
   return check_hip(e, "paged attention launch");

@@ -241,7 +241,8 @@ __device__ __forceinline__ Piece next_piece(const PagedAttnArgs& a, const Share&
   return {from < 0 ? 0 : from, to < 0 ? 0 : to, units, (x - at + a.extra + tiles - 1) / w.tiles};
 }
 
-template <bool F16, int DH, int NW, bool CAP, bool BIAS>
+// FAR: the cap is above kNearCap.
+template <bool F16, int DH, int NW, bool CAP, bool BIAS, bool FAR>
 __global__ __launch_bounds__(64 * NW, DH == 256 ? 1 : (NW == 4 ? 2 : 1)) void paged_attention_kernel(PagedAttnArgs a) {
   constexpr bool MOD = CAP || BIAS;   // scores are brought to base-2 units before the softmax
   using ST = Storage<F16>;
@@ -413,8 +414,13 @@ __global__ __launch_bounds__(64 * NW, DH == 256 ? 1 : (NW == 4 ? 2 : 1)) void pa
     // Scores are in base-2 units with MOD, else still to be multiplied by scale * log2(e).
     // Register r of s[kb] is row 32 * kb + 8 * (r / 4) + 4 * h + r % 4 of the tile.
     auto base2_scores = [&](floatx16 (&s)[2]) {
-      if constexpr (CAP) {
-        // cap * tanh(x) = cap * (1 - 2 / (1 + e^(2x))): off by cap * 2^-23 at most, which a probability's rounding to 16 bits covers
+      if constexpr (FAR) {
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) s[kb][r] = sc.cap_log2e * tanh_of(s[kb][r] * sc.cap_in);
+      } else if constexpr (CAP) {
+        // cap * tanh(x) = cap * (1 - 2 / (1 + e^(2x)))
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
@@ -894,9 +900,9 @@ hipError_t launch_paged_join(const PagedAttnArgs& a, hipStream_t s) {
   return hipGetLastError();
 }
 
-template <bool F16, int DH, int NW, bool CAP, bool BIAS>
+template <bool F16, int DH, int NW, bool CAP, bool BIAS, bool FAR = false>
 hipError_t launch_paged_one(const PagedAttnArgs& a, hipStream_t s) {
-  auto kern = paged_attention_kernel<F16, DH, NW, CAP, BIAS>;
+  auto kern = paged_attention_kernel<F16, DH, NW, CAP, BIAS, FAR>;
   static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize,
                                                      PagedSmem<DH>::BYTES);
   if (attr != hipSuccess) return attr;
@@ -905,19 +911,23 @@ hipError_t launch_paged_one(const PagedAttnArgs& a, hipStream_t s) {
   return e != hipSuccess || a.cut == nullptr ? e : launch_paged_join<F16, DH>(a, s);
 }
 
-template <bool F16, int DH, int NW>
+template <bool F16, int DH, int NW, bool FAR>
 hipError_t launch_paged_waves(const PagedAttnArgs& a, hipStream_t s) {
-  if (a.sc.cap_log2e > 0.f)
-    return a.sc.slopes != nullptr ? launch_paged_one<F16, DH, NW, true, true>(a, s) : launch_paged_one<F16, DH, NW, true, false>(a, s);
-  return a.sc.slopes != nullptr ? launch_paged_one<F16, DH, NW, false, true>(a, s) : launch_paged_one<F16, DH, NW, false, false>(a, s);
+  if constexpr (FAR) {
+    return a.sc.slopes != nullptr ? launch_paged_one<F16, DH, NW, true, true, true>(a, s) : launch_paged_one<F16, DH, NW, true, false, true>(a, s);
+  } else {
+    if (a.sc.cap_log2e > 0.f)
+      return a.sc.slopes != nullptr ? launch_paged_one<F16, DH, NW, true, true>(a, s) : launch_paged_one<F16, DH, NW, true, false>(a, s);
+    return a.sc.slopes != nullptr ? launch_paged_one<F16, DH, NW, false, true>(a, s) : launch_paged_one<F16, DH, NW, false, false>(a, s);
+  }
 }
 
-template <bool F16, int DH>
+template <bool F16, int DH, bool FAR = false>
 hipError_t launch_paged(const PagedAttnArgs& a, int waves, hipStream_t s) {
   if constexpr (DH != 256) {   // (heads of 256 leave no registers for two wavefronts on a SIMD)
-    if (waves == 8) return launch_paged_waves<F16, DH, 8>(a, s);
+    if (waves == 8) return launch_paged_waves<F16, DH, 8, FAR>(a, s);
   }
-  return launch_paged_waves<F16, DH, 4>(a, s);
+  return launch_paged_waves<F16, DH, 4, FAR>(a, s);
 }
 
 }  // namespace

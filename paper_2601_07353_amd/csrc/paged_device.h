@@ -10,6 +10,19 @@ constexpr float kNoScore = -__builtin_huge_valf();
 constexpr float kLog2eF = 1.4426950408889634f;
 constexpr float kLn2F = 0.6931471805599453f;
 
+// tanh(x) to a few units in the last place, also near 0, where 1 - 2 / (1 + e^(2x)) keeps no more than its absolute accuracy
+// (scores of large caps, and the weights, whose sums stay in fp32, need better): the continued fraction x / (1 + x^2 / (3 + x^2 / (5 + ...)))
+// of Lambert, cut behind 13 and written as a quotient; its error is below 2^-24 for |x| <= 2, beyond the other form is exact.
+__device__ __forceinline__ float tanh_of(float x) {
+  const float u = x * x;
+  const float num = __builtin_fmaf(__builtin_fmaf(u + 378.f, u, 17325.f), u, 135135.f);
+  const float den = __builtin_fmaf(__builtin_fmaf(__builtin_fmaf(28.f, u, 3150.f), u, 62370.f), u, 135135.f);
+  const float small = x * (num * __builtin_amdgcn_rcpf(den));
+  const float e = __builtin_amdgcn_exp2f(x * (2.f * kLog2eF));
+  const float large = __builtin_fmaf(-2.f, __builtin_amdgcn_rcpf(1.f + e), 1.f);
+  return fabsf(x) <= 2.f ? small : large;
+}
+
 // x / G for 0 <= x < 2^24, G <= 128: exact, since x * (inv_g * G - 2^32) < 2^32.
 // (inv_g is 0 for G = 1; without a branch, which would end a block.)
 __device__ __forceinline__ int div_g(int x, uint32_t inv_g) {

@@ -32,7 +32,7 @@ __device__ __forceinline__ void wait_loads() {   // until at most N loads are on
   asm volatile("s_waitcnt vmcnt(%0)" :: "n"(N) : "memory");
 }
 
-template <bool F16, int DH, bool CAP, bool BIAS>
+template <bool F16, int DH, bool CAP, bool BIAS, bool FAR>
 __global__ __launch_bounds__(64 * FewSmem<DH>::NW, DH == 256 ? 1 : 2) void paged_few_kernel(PagedAttnArgs a) {
   using ST = Storage<F16>;
   using x8 = typename ST::x8;
@@ -194,7 +194,10 @@ __global__ __launch_bounds__(64 * FewSmem<DH>::NW, DH == 256 ? 1 : 2) void paged
         reads_done();
         load_k();
       }
-      if constexpr (CAP) {   // (see paged_attention.h)
+      if constexpr (FAR) {   // (see paged_attention.h)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[r] = sc.cap_log2e * tanh_of(s[r] * sc.cap_in);
+      } else if constexpr (CAP) {
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
           const float e = __builtin_amdgcn_exp2f(s[r] * sc.cap_in);
@@ -395,9 +398,9 @@ __global__ __launch_bounds__(64 * FewSmem<DH>::NW, DH == 256 ? 1 : 2) void paged
   }
 }
 
-template <bool F16, int DH, bool CAP, bool BIAS>
+template <bool F16, int DH, bool CAP, bool BIAS, bool FAR = false>
 hipError_t launch_few_one(const PagedAttnArgs& a, hipStream_t s) {
-  auto kern = paged_few_kernel<F16, DH, CAP, BIAS>;
+  auto kern = paged_few_kernel<F16, DH, CAP, BIAS, FAR>;
   static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize,
                                                      FewSmem<DH>::BYTES);
   if (attr != hipSuccess) return attr;
@@ -406,10 +409,14 @@ hipError_t launch_few_one(const PagedAttnArgs& a, hipStream_t s) {
   return e != hipSuccess || a.cut == nullptr ? e : launch_paged_join<F16, DH>(a, s);
 }
 
-template <bool F16, int DH>
+template <bool F16, int DH, bool FAR = false>
 hipError_t launch_few(const PagedAttnArgs& a, hipStream_t s) {
-  if (a.sc.cap_log2e > 0.f) return a.sc.slopes != nullptr ? launch_few_one<F16, DH, true, true>(a, s) : launch_few_one<F16, DH, true, false>(a, s);
-  return a.sc.slopes != nullptr ? launch_few_one<F16, DH, false, true>(a, s) : launch_few_one<F16, DH, false, false>(a, s);
+  if constexpr (FAR) {
+    return a.sc.slopes != nullptr ? launch_few_one<F16, DH, true, true, true>(a, s) : launch_few_one<F16, DH, true, false, true>(a, s);
+  } else {
+    if (a.sc.cap_log2e > 0.f) return a.sc.slopes != nullptr ? launch_few_one<F16, DH, true, true>(a, s) : launch_few_one<F16, DH, true, false>(a, s);
+    return a.sc.slopes != nullptr ? launch_few_one<F16, DH, false, true>(a, s) : launch_few_one<F16, DH, false, false>(a, s);
+  }
 }
 
 }  // namespace

@@ -27,6 +27,12 @@ struct RowsView {            // [B][N][H][Dh] of a caller's tensor, strides in e
   int64_t sb, st, sh;
 };
 
+// Caps up to here are formed by one exponential and a reciprocal in attention (cap - 2 cap / (1 + e^(2x))), which is off by 2^-22 of
+// the cap near a score of 0: 2^-16 at most, a 32nd of the half step that a probability is rounded by in fp16, and no more than four times the
+// spacing of fp32 numbers near the cap.  Larger ones have kernels of their own, with tanh_of(): a chunk of
+// 2048 tokens at 8192 rows, 32/8 heads of 128, 652 us against 394, 4 trees of 128 nodes 78 against 56, 8 tokens at 8192 rows 52.6 against 50.8.
+constexpr float kNearCap = 64.f;
+
 // What decides a score besides the product (attention and its weights alike).
 struct ScoreArgs {
   const int32_t* n_new;      // [B]
@@ -37,7 +43,7 @@ struct ScoreArgs {
   int N, words, max_prefix_len, window;
   float scale_log2e;         // scale * log2(e)
   float cap_log2e;           // cap * log2(e); 0: none
-  float cap_in;              // with x = scale * product / cap: 2 x log2(e) / product in attention, x / product in the weights
+  float cap_in;              // with x = scale * product / cap: 2 x log2(e) / product in attention up to kNearCap, else x / product
 };
 
 struct PagedAttnArgs {
@@ -110,6 +116,8 @@ hipError_t launch_paged_attention_bf16_256(const PagedAttnArgs& a, int waves, hi
 hipError_t launch_paged_attention_f16_64(const PagedAttnArgs& a, int waves, hipStream_t s);
 hipError_t launch_paged_attention_f16_128(const PagedAttnArgs& a, int waves, hipStream_t s);
 hipError_t launch_paged_attention_f16_256(const PagedAttnArgs& a, int waves, hipStream_t s);
+hipError_t launch_paged_attention_bf16_far(const PagedAttnArgs& a, int Dh, int waves, hipStream_t s);   // caps above kNearCap
+hipError_t launch_paged_attention_f16_far(const PagedAttnArgs& a, int Dh, int waves, hipStream_t s);
 hipError_t launch_paged_weights_bf16(const PagedWeightArgs& wa, int Dh, bool few, hipStream_t s);
 hipError_t launch_paged_weights_f16(const PagedWeightArgs& wa, int Dh, bool few, hipStream_t s);
 hipError_t launch_rotary_store(const RotaryArgs& a, int dtype, hipStream_t s);

@@ -17,19 +17,6 @@ namespace talon {
 
 namespace {
 
-// tanh(x) to a few units in the last place, also near 0, where 1 - 2 / (1 + e^(2x)) keeps no more than its absolute accuracy
-// (the sums here stay in fp32, so the scores have to be as good): the continued fraction x / (1 + x^2 / (3 + x^2 / (5 + ...)))
-// of Lambert, cut behind 13 and written as a quotient; its error is below 2^-24 for |x| <= 2, beyond the other form is exact.
-__device__ __forceinline__ float tanh_of(float x) {
-  const float u = x * x;
-  const float num = __builtin_fmaf(__builtin_fmaf(u + 378.f, u, 17325.f), u, 135135.f);
-  const float den = __builtin_fmaf(__builtin_fmaf(__builtin_fmaf(28.f, u, 3150.f), u, 62370.f), u, 135135.f);
-  const float small = x * (num * __builtin_amdgcn_rcpf(den));
-  const float e = __builtin_amdgcn_exp2f(x * (2.f * kLog2eF));
-  const float large = __builtin_fmaf(-2.f, __builtin_amdgcn_rcpf(1.f + e), 1.f);
-  return fabsf(x) <= 2.f ? small : large;
-}
-
 // Whether new token i sees row `key` (at position `pos`), but for the window.
 __device__ __forceinline__ bool sees_row(const ScoreArgs& s, int b, int i, int P, int key) {
   if (key < P) return true;
