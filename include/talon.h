@@ -529,7 +529,7 @@ typedef struct talon_scores {
   const int32_t* offset;    /* [B][N], between 0 and 2^30 - 1 (else the nearest); NULL: i                     */
   const float* slopes;      /* [Hq] or NULL                                                      */
   float scale;              /* 0: 1/sqrt(Dh)                                                     */
-  float softcap;            /* 0: none                                                           */
+  float softcap;            /* 0: none; scale / softcap must be a normal number                  */
   int32_t window;           /* 0: none                                                           */
 } talon_scores;
 

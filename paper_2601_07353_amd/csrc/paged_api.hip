@@ -95,6 +95,14 @@ int check_scores(const talon_scores* s, int N, int Dh, int max_prefix_len, const
   if (s->window < 0) { set_error("window=%d must be >= 0 (0: none)", s->window); return TALON_ERR_INVALID_ARG; }
   const double scale = s->scale == 0.f ? 1.0 / sqrt(static_cast<double>(Dh)) : static_cast<double>(s->scale);
   const double log2e = 1.4426950408889634;
+  // What the kernels multiply by has to be a number in 32 bits: a score of 0 times infinity is none, and a quotient below the least normal
+  // number has lost its digits.
+  auto held = [](double x) { return fabs(x) <= 3.4028234e38; };
+  if (!held(scale * log2e) || !held(s->softcap * log2e) ||
+      (s->softcap > 0.f && (!held(2.0 * scale * log2e / s->softcap) || scale / s->softcap < 1.1754944e-38))) {
+    set_error("scale=%g with softcap=%g: the products with log2(e) and the quotient must be normal 32-bit numbers", scale, static_cast<double>(s->softcap));
+    return TALON_ERR_INVALID_ARG;
+  }
   out->n_new = n_new; out->prefix_len = prefix_len; out->mask = s->mask; out->offset = s->offset; out->slopes = s->slopes;
   out->N = N; out->words = (N + 63) / 64; out->max_prefix_len = max_prefix_len; out->window = s->window;
   out->scale_log2e = static_cast<float>(scale * log2e);
