@@ -260,13 +260,13 @@ int talon_paged_evict(const talon_paged_cache* cache, const talon_paged_cache* d
     set_error("weights: a stride does not hold the rows");
     return TALON_ERR_INVALID_ARG;
   }
-  if (new_weights == weights && (new_stride_b != stride_b || new_stride_h != stride_h)) { set_error("weights in place need one set of strides"); return TALON_ERR_INVALID_ARG; }
+  if (new_weights == weights && ((B > 1 && new_stride_b != stride_b) || (Hkv > 1 && new_stride_h != stride_h))) { set_error("weights in place need one set of strides"); return TALON_ERR_INVALID_ARG; }
   a.len = len; a.new_len = new_len; a.weights = weights; a.new_weights = new_weights;
   a.stride_b = stride_b; a.stride_h = stride_h; a.new_stride_b = new_stride_b; a.new_stride_h = new_stride_h;
   a.kept = kept; a.B = B; a.Hkv = Hkv; a.Dh = cache->Dh; a.budget = budget; a.n_sink = n_sink; a.n_recent = n_recent; a.max_len = max_len;
   a.in_place = dst->page_table == cache->page_table && dst->k == cache->k && dst->v == cache->v;
   if (a.in_place && (dst->page_size != cache->page_size || dst->max_pages != cache->max_pages || dst->num_pages != cache->num_pages ||
-                     dst->stride_page != cache->stride_page || dst->stride_token != cache->stride_token || dst->stride_head != cache->stride_head)) {
+                     a.dst.page_chunks != a.src.page_chunks || a.dst.token_chunks != a.src.token_chunks || a.dst.head_chunks != a.src.head_chunks)) {
     set_error("dst in place must be the same cache");
     return TALON_ERR_INVALID_ARG;
   }
