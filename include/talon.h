@@ -575,8 +575,8 @@ int talon_paged_attention(const talon_paged_cache* cache, const talon_view* q, i
  * The attention weight that every row of the cache receives, added up (what talon_paged_evict goes by):
  *   weights[b][g][j] = decay * prior[b][g][j] (j < prefix_len[b]) + sum over new tokens i and query heads h of
  *                      KV head g of exp(x_ihj - lse[b][i][h]),   j < prefix_len[b] + n_new[b]
- * with scores and arguments as in talon_paged_attention and its out_lse; a token whose lse is +inf counts nothing
- * (a drafted token that was not accepted).  weights, prior float, element (b, g, j) at b*stride_b + g*stride_h + j;
+ * with scores and arguments as in talon_paged_attention and its out_lse; a token whose lse is +inf counts nothing,
+ * whatever its query holds (a drafted token that was not accepted).  weights, prior float, element (b, g, j) at b*stride_b + g*stride_h + j;
  * prior may be weights or NULL (0); further rows are untouched.  Sums are fp32, in a fixed order.
  *   Errors: as talon_paged_attention (no workspace), INVALID_ARG for strides that do not hold max_prefix_len + N rows
  *   (or the table's rows where those are fewer) and for decay outside [-1, 1].

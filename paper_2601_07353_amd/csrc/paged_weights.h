@@ -25,7 +25,7 @@ __device__ __forceinline__ bool sees_row(const ScoreArgs& s, int b, int i, int P
   return (s.mask[(static_cast<size_t>(b) * s.N + i) * s.words + (d >> 6)] >> (d & 63)) & 1u;
 }
 
-constexpr int kNobody = -1;   // token of a row behind the last query
+constexpr int kNobody = -1;   // token of a row that counts nothing: behind the last query, or of a token whose lse is +inf
 
 constexpr int kQueryTile = 128;
 
@@ -38,10 +38,11 @@ struct QueryTables {
 };
 
 // Sum over the 16 queries of this half in a 32 x 32 block of products: register r is query 8 * (r / 4) + 4 * h + r % 4.  `whole`: each
-// of them sees each key of the block; `count` queries there are.
+// of them sees each key of the block; `everyone`: each of the `count` queries that there are counts.  (One that does not may have any
+// score, a NaN too: x = score - inf is not relied on.)
 template <bool CAP, bool BIAS>
-__device__ __forceinline__ float block_sum(const PagedAttnArgs& a, floatx16 s, const QueryTables& t, int q0, int h, bool whole, int b, int P, int key, int pos,
-                                           bool real, int count) {
+__device__ __forceinline__ float block_sum(const PagedAttnArgs& a, floatx16 s, const QueryTables& t, int q0, int h, bool whole, bool everyone, int b, int P, int key,
+                                           int pos, bool real, int count) {
   const ScoreArgs& sc = a.sc;
   if constexpr (CAP) {
 #pragma unroll
@@ -65,13 +66,22 @@ __device__ __forceinline__ float block_sum(const PagedAttnArgs& a, floatx16 s, c
     }
   }
   float sum[4] = {0.f, 0.f, 0.f, 0.f};
-  if (whole && count == 32) {   // uniform; nothing else in the way of the exponentials
+  if (whole && everyone && count == 32) {   // uniform; nothing else in the way of the exponentials
 #pragma unroll
     for (int r = 0; r < 16; ++r) sum[r % 4] += __builtin_amdgcn_exp2f(x[r]);
-  } else if (whole) {
+  } else if (whole && everyone) {
 #pragma unroll
     for (int r = 0; r < 16; ++r)
       if (8 * (r / 4) < count) sum[r % 4] += 8 * (r / 4) + 4 * h + r % 4 < count ? __builtin_amdgcn_exp2f(x[r]) : 0.f;
+  } else if (whole) {
+#pragma unroll
+    for (int q4 = 0; q4 < 4; ++q4) {
+      if (8 * q4 >= count) continue;
+      const int4 t4 = *reinterpret_cast<const int4*>(&t.token[q0 + 8 * q4 + 4 * h]);
+      const int ts[4] = {t4.x, t4.y, t4.z, t4.w};
+#pragma unroll
+      for (int e = 0; e < 4; ++e) sum[e] += ts[e] != kNobody ? __builtin_amdgcn_exp2f(x[4 * q4 + e]) : 0.f;
+    }
   } else {
     const int window = sc.window > 0 ? sc.window : 0x7FFFFFFF;
 #pragma unroll
@@ -204,7 +214,7 @@ __global__ __launch_bounds__(512, DH == 256 ? 2 : 4) void paged_weights_kernel(P
   auto store_tables = [&](int st) {
     if (tid < QT) {
       s_t[st].lse[tid] = lse_next * kLog2eF;
-      s_t[st].token[tid] = token_next;
+      s_t[st].token[tid] = lse_next == __builtin_huge_valf() ? kNobody : token_next;
       s_t[st].pos[tid] = P + (off_next < 0 ? 0 : (off_next < kMostOffset ? off_next : kMostOffset));
       if constexpr (BIAS) s_t[st].slope[tid] = slope_next * kLog2eF;
     }
@@ -231,12 +241,13 @@ __global__ __launch_bounds__(512, DH == 256 ? 2 : 4) void paged_weights_kernel(P
     for (int r = 0; r < 16; ++r) s[r] = 0.f;
     const int row = q0 + l32;
     const int swz = SM::kswz(row);
+    const bool everyone = __ballot(s_t[st].token[row] == kNobody) == 0ull;
 #pragma unroll
     for (int ds = 0; ds < DSTEPS; ++ds) {
       const x8 aq = __builtin_bit_cast(x8, *reinterpret_cast<const uint4*>(smem + st * WeighSmem<DH>::STAGE + row * DH + ((2 * ds + h) ^ swz) * 8));
       s = ST::mfma(aq, bk[ds], s);
     }
-    acc += block_sum<CAP, BIAS>(a, s, s_t[st], q0, h, whole, b, P, key, pos, real, 32);
+    acc += block_sum<CAP, BIAS>(a, s, s_t[st], q0, h, whole, everyone, b, P, key, pos, real, 32);
     if ((count & 15) == 0) {
       sum += acc;
       acc = 0.f;
@@ -340,6 +351,7 @@ __global__ __launch_bounds__(64 * WeighFewSmem<DH>::NW, DH == 256 ? 1 : 2) void 
 
     // ---- the queries, their denominators and places
     x8 aq[DSTEPS];
+    bool everyone;
     {
       const bool valid = l32 < rows;
       const int token = valid ? div_g(l32, a.inv_g) : 0;
@@ -351,9 +363,11 @@ __global__ __launch_bounds__(64 * WeighFewSmem<DH>::NW, DH == 256 ? 1 : 2) void 
         qv[ds] = u32x4{0, 0, 0, 0};
         if (valid) qv[ds] = *reinterpret_cast<const u32x4*>(qp + 16 * ds);
       }
+      float lse = __builtin_huge_valf();
       if (h == 0) {
-        s_t.lse[l32] = valid ? a.lse[(static_cast<size_t>(b) * sc.N + token) * (a.Hkv * G) + head] * kLog2eF : __builtin_huge_valf();
-        s_t.token[l32] = valid ? token : kNobody;
+        if (valid) lse = a.lse[(static_cast<size_t>(b) * sc.N + token) * (a.Hkv * G) + head];
+        s_t.lse[l32] = lse * kLog2eF;
+        s_t.token[l32] = lse == __builtin_huge_valf() ? kNobody : token;
         s_t.pos[l32] = P + offset_of(sc, b, token);
         if constexpr (BIAS) s_t.slope[l32] = valid ? sc.slopes[head] * kLog2eF : 0.f;
       }
@@ -362,6 +376,7 @@ __global__ __launch_bounds__(64 * WeighFewSmem<DH>::NW, DH == 256 ? 1 : 2) void 
       for (int ds = 0; ds < DSTEPS; ds += 4) asm volatile("" : "+v"(qv[ds]), "+v"(qv[ds + 1]), "+v"(qv[ds + 2]), "+v"(qv[ds + 3]));
 #pragma unroll
       for (int ds = 0; ds < DSTEPS; ++ds) aq[ds] = __builtin_bit_cast(x8, qv[ds]);
+      everyone = __ballot(h == 0 && valid && lse == __builtin_huge_valf()) == 0ull;
       __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
       __builtin_amdgcn_wave_barrier();
     }
@@ -394,7 +409,7 @@ __global__ __launch_bounds__(64 * WeighFewSmem<DH>::NW, DH == 256 ? 1 : 2) void 
       const float before = loads_prior ? s_prior[st * 64 + l32] : 0.f;
       // every query sees the tile whole where it lies in the prefix and nothing hides it (rows without a query have weight 0)
       const bool whole = (t + 1) * 32 <= P && sc.window == 0;
-      const float total = both_halves(block_sum<CAP, BIAS>(a, s, s_t, 0, h, whole, b, P, key, pos, real, rows));
+      const float total = both_halves(block_sum<CAP, BIAS>(a, s, s_t, 0, h, whole, everyone, b, P, key, pos, real, rows));
       if (h == 0 && real) out[key] = total + (key < P ? wa.decay * before : 0.f);
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // the stage is free
       if (t + 2 < t_end) load_tile(t + 2, st);
