@@ -576,10 +576,10 @@ int talon_paged_attention(const talon_paged_cache* cache, const talon_view* q, i
  *   weights[b][g][j] = decay * prior[b][g][j] (j < prefix_len[b]) + sum over new tokens i and query heads h of
  *                      KV head g of exp(x_ihj - lse[b][i][h]),   j < prefix_len[b] + n_new[b]
  * with scores and arguments as in talon_paged_attention and its out_lse; a token whose lse is +inf counts nothing,
- * whatever its query holds (a drafted token that was not accepted).  weights, prior float, element (b, g, j) at b*stride_b + g*stride_h + j;
- * prior may be weights or NULL (0); further rows are untouched.  Sums are fp32, in a fixed order.
- *   Errors: as talon_paged_attention (no workspace), INVALID_ARG for strides that do not hold max_prefix_len + N rows
- *   (or the table's rows where those are fewer) and for decay outside [-1, 1].
+ * whatever its query holds (a drafted token that was not accepted).  weights, prior float, element (b, g, j) at b*stride_b +
+ * g*stride_h + j; prior may be weights or NULL (0); further rows are untouched.  Sums are fp32, in a fixed order.
+ *   Errors: as talon_paged_attention (no workspace), UNSUPPORTED for nearly 2^29 rows and more where N * Hq / Hkv > 32, INVALID_ARG
+ *   for strides that do not hold max_prefix_len + N rows (or the table's rows where those are fewer) and for decay outside [-1, 1].
  */
 int talon_paged_weights(const talon_paged_cache* cache, const talon_view* q, int32_t N, int32_t Hq, const int32_t* n_new,
                         const int32_t* prefix_len, int32_t max_prefix_len, const talon_scores* scores, const float* lse,

@@ -221,6 +221,10 @@ int talon_paged_weights(const talon_paged_cache* cache, const talon_view* q, int
   a.B = B; a.Hkv = Hkv; a.G = Hq / Hkv; a.inv_g = inverse_of(a.G);
   wa.prior = prior; wa.out = weights; wa.stride_b = stride_b; wa.stride_h = stride_h; wa.decay = decay;
   const bool few = static_cast<long long>(N) * a.G <= 32;
+  if (!few && (most + kWeighRows - 1) / kWeighRows * kWeighThreads >= 1ll << 32) {   // (the threads of a grid's dimension)
+    set_error("%lld rows for more than 32 queries of a KV head are not supported", most);
+    return TALON_ERR_UNSUPPORTED;
+  }
   const WeighPlan p = weigh_plan(B, Hkv, Dh, static_cast<int>(most));
   if (p.tiles >= 1ll << 30) { set_error("%lld key tiles are more than one call takes", p.tiles); return TALON_ERR_UNSUPPORTED; }
   a.split = 1; a.slots = p.slots; a.least = p.least; a.extra = p.extra;

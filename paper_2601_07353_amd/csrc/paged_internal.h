@@ -64,6 +64,9 @@ struct PagedAttnArgs {
   int4* cut;                 // [slots] the row tile that a share's end cuts, see paged_attention.h; NULL: nothing is joined
 };
 
+// Weights of many queries: rows of the cache of a workgroup, and its threads.
+constexpr int kWeighRows = 64, kWeighThreads = 512;
+
 struct PagedWeightArgs {
   PagedAttnArgs a;           // cache, scores, queries, lse (read), shares
   const float* prior;        // or NULL

@@ -111,7 +111,6 @@ __device__ __forceinline__ float both_halves(float v) {
 // the matrix product, which hardly run at the same time.  The time of a workgroup is short against the call's, so that the last
 // ones cost little: 512 tokens at 8192 rows 71 us, against 77 with four wavefronts and tiles of 64 rows and 82 with four wavefronts
 // on 128 rows.
-constexpr int kWeighRows = 64;
 
 template <int DH>
 struct WeighSmem {
@@ -120,7 +119,7 @@ struct WeighSmem {
 };
 
 template <bool F16, int DH, bool CAP, bool BIAS>
-__global__ __launch_bounds__(512, DH == 256 ? 2 : 4) void paged_weights_kernel(PagedWeightArgs wa) {
+__global__ __launch_bounds__(kWeighThreads, DH == 256 ? 2 : 4) void paged_weights_kernel(PagedWeightArgs wa) {
   using ST = Storage<F16>;
   using x8 = typename ST::x8;
   using SM = PagedSmem<DH>;
@@ -442,7 +441,7 @@ hipError_t launch_weights_one(const PagedWeightArgs& wa, bool few, hipStream_t s
     static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize,
                                                        WeighSmem<DH>::BYTES);
     if (attr != hipSuccess) return attr;
-    hipLaunchKernelGGL(kern, dim3((most + kWeighRows - 1) / kWeighRows, wa.a.Hkv, wa.a.B), dim3(512), WeighSmem<DH>::BYTES, s, wa);
+    hipLaunchKernelGGL(kern, dim3((most + kWeighRows - 1) / kWeighRows, wa.a.Hkv, wa.a.B), dim3(kWeighThreads), WeighSmem<DH>::BYTES, s, wa);
   }
   return hipGetLastError();
 }

@@ -33,3 +33,13 @@ def test_refused(name, scale, cap):
 def test_not_refused(name, scale, cap):
     rc, said = call(name, scale, cap)
     assert (rc, "workspace" in said) == (T.TALON_ERR_WORKSPACE, True) if name == "attention" else "lse / weights is NULL" in said, said
+
+
+def test_weights_of_more_rows_than_a_launch_covers():
+    """Many queries over 2^29 rows and more: a workgroup of 512 threads for 64 of them is 2^32 threads, refused like other sizes."""
+    lib = T.load_library()
+    c = ctypes.byref(_CPagedCache(1, 1, 64, 1, 64, 1 << 20, 1024, 64 << 20, 64, 64, P, P + 0x1000000, P + 4, P + 8))
+    v = ctypes.byref(_CView(P, 0, 64, 64))
+    for most in ((1 << 29), (1 << 30)):
+        rc = lib.talon_paged_weights(c, v, 33, 1, P, P, most, None, P, 1.0, None, P, 1 << 30, 1 << 30, None)
+        assert rc == T.TALON_ERR_UNSUPPORTED and "rows" in lib.talon_last_error_string().decode()
