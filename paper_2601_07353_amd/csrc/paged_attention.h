@@ -113,6 +113,19 @@ __device__ __forceinline__ int tiles_of(const ScoreArgs& sc, int P, int n, uint3
   return (end + TILE - 1) / TILE - begin / TILE;
 }
 
+// Rows beyond the page tables, reported by the workgroup of the last share, which has the least to do, if anything.  The kernels of few
+// rows do it in find_share behind the lengths (in front of it: 0.3 us of one token's 10), that of many rows in front of it (behind the
+// lengths: 2 % of 16 trees of 256 nodes at 16384 rows, through the loop's registers); beside the lengths that every workgroup looks at, it
+// took 0.3 to 0.6 us of all calls over short prefixes, in instructions that are not in the cache yet.
+__device__ __forceinline__ void report_table_ends(const PagedAttnArgs& a) {
+  if (__builtin_expect(blockIdx.x == gridDim.x - 1, 0)) {
+    const ScoreArgs& sc = a.sc;
+#pragma unroll 1
+    for (int b = static_cast<int>(threadIdx.x); b < a.B; b += static_cast<int>(blockDim.x))
+      report_table_end(a.c, b, sc.prefix_len[b], sc.n_new[b], sc.max_prefix_len, sc.N);
+  }
+}
+
 // A workgroup's share of the line of key tiles: [x, x_end), which begins with tile `at` of row tile rt of (b, g).  Or a piece of one
 // row tile, `take` tiles from `at` on, the last one of which has share `last`.
 struct Share {
@@ -159,13 +172,7 @@ __device__ __forceinline__ bool find_share(const PagedAttnArgs& a, int lane, Sha
     total_l += sum;
     pieces_l += pieces;
   }
-  // Rows beyond the page tables are reported by the workgroup that has least to do, if anything.  (Beside the lengths that all of them
-  // look at, the check took 0.3 to 0.6 us of a call over short prefixes, in instructions that are not in the cache yet.)
-  if (__builtin_expect(share == static_cast<int>(gridDim.x) - 1, 0)) {
-#pragma unroll 1
-    for (int bb = static_cast<int>(threadIdx.x); bb < a.B; bb += static_cast<int>(blockDim.x))
-      report_table_end(a.c, bb, sc.prefix_len[bb], sc.n_new[bb], sc.max_prefix_len, sc.N);
-  }
+  if constexpr (ROW_TILE == 32) report_table_ends(a);
   int total = uniform(wave_sum_i32(total_l));   // of tiles and what row tiles cost besides them
   int tiles = (total + a.slots - 1) / a.slots;
   // Little work: pieces of single row tiles, no share with two of them (and their two prologues)
@@ -269,6 +276,7 @@ __global__ __launch_bounds__(64 * NW, DH == 256 ? 1 : (NW == 4 ? 2 : 1)) void pa
   const ScoreArgs& sc = a.sc;
   const int G = a.G;
 
+  report_table_ends(a);
   Share w;
   if (!find_share<kTileRows, kRowTile>(a, lane, &w)) return;
   int b = w.b, g = w.g, rt = w.rt, at = w.at, x = w.x, P = w.P, n = w.n;
