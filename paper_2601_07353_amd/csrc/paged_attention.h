@@ -14,8 +14,8 @@
 // so that the accumulators of S^T are the operand P^T of the second product as they stand, and the statistics of a row are
 // scalars of a lane.  While the matrix pipe forms the scores of tile t + 1 the vector pipe takes the exponentials of tile t.
 // Bound: those two, which share a SIMD's issue slots; the step's barrier and the wait for its loads.  Two chunks of 2048 tokens at
-// 8192 rows, 32/8 heads of 128, 629 us (980 TFLOP/s; 760 us capped, 701 with distances, 877 with both); one at 4096 rows, 16/4
-// heads of 256 (one wavefront per SIMD), 325 us (530 TFLOP/s; 486 with the tiles one after the other).
+// 8192 rows, 32/8 heads of 128, 661 us (936 TFLOP/s; 795 us capped, 735 with distances, 913 with both); one at 4096 rows, 16/4
+// heads of 256 (one wavefront per SIMD), 308 us (558 TFLOP/s; 486 us with the tiles one after the other).
 //
 // Work.  Every (sequence, KV head, row tile) needs a number of key tiles that the host does not know (lengths are on the
 // device).  All of them, end to end in that order, are one line of W tiles, cut into equal shares of ceil(W / workgroups), at
